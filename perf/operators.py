@@ -474,10 +474,11 @@ def run(st):
                           *st["users"], 0, ctx_k=st["ck"], ctx_w=st["cw"], ctx_w_prior=st["cw0"], res_k=st["rk"],
                           res_w=st["rw"], res_w_prior=st["rw0"], res_off=st["res_off"])
         return [st["rw"], st["cw"]]
+    route_off, route_res, route_tokens = st["route"]
     rc.attend_quantized(st["q"], st["ck"], st["cv"], st["ck_exp"], st["cv_exp"], st["cu_q"], st["cu_ctx"], st["max_q"],
-                        st["max_ctx"], st["rk"], st["rv"], st["rk_exp"], st["rv_exp"], st["cu_kept"], *st["route"], 0, 1,
-                        st["out"], ctx_len=st["len"], max_route_len=case["per_req"], max_kv=st["max_kv"],
-                        workspace=st["ws"], res_off=st["res_off"])
+                        st["max_ctx"], st["rk"], st["rv"], st["rk_exp"], st["rv_exp"], st["cu_kept"], route_off,
+                        route_res, route_tokens.view(-1), 0, 1, st["out"], ctx_len=st["len"],
+                        max_route_len=case["per_req"], max_kv=st["max_kv"], workspace=st["ws"], res_off=st["res_off"])
     return [st["out"]]
 
 
