@@ -23,6 +23,12 @@
  *                                      ReCache mask, Fig. 2)
  *   recache_select_routes              [host] Omega* = L* x G* from contribution
  *                                      scores, with sparsity and coverage
+ *   recache_resource_users /           attention weight that every cached row has
+ *   recache_attend_weights             received, and
+ *   recache_select_kept                the kept lists that it makes: eviction
+ *   recache_quantize_kv                K/V rows into 8-bit caches (e4m3, a power of
+ *                                      two per 64 tokens and KV head)
+ *   recache_attend_quantized           recache_attend_cached over such caches
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -400,6 +406,165 @@ int recache_attend_cached_noalloc(int dtype, int layer, int n_layers, int n_req,
 int recache_select_routes(int n_layers, int n_groups, const double* s_layer, const double* s_group,
                           int k_layers, int k_groups, uint8_t* route_mask, double* w_layer,
                           double* w_group, double* rho, double* cc_layer, double* cc_group);
+
+/*
+ * Eviction by accumulated attention weight (library convention; Sec. 3,
+ * "Semantic Pruning", takes the kept tokens of a resource as given).  The
+ * calls below make kept lists from what the conversation attended to:
+ *   recache_attend_cached with lse, recache_attend_weights per layer and step
+ *   into one array, recache_select_kept, then recache_prune_gather (or
+ *   recache_store_routes, recache_build_routes) with its lists.
+ * The rows of a conversation's context are evicted the same way, as segments
+ * cu_ctx.
+ */
+
+/*
+ * The inverse of the request lists of recache_build_routes, built once per
+ * batch: user_req[user_off[r] .. user_off[r+1]) are the requests that list
+ * resource r, in request order (once for every time that a request lists it).
+ *   user_off[n_res + 1], user_req[total_req_res] int32 (device)
+ * Exact and deterministic.  A resource outside [0, n_res) has no users.
+ * Errors: RECACHE_EINVAL for bad sizes or null pointers.
+ */
+int recache_resource_users(int n_req, const int32_t* req_res_off, const int32_t* req_res,
+                           int total_req_res, int n_res, int32_t* user_off, int32_t* user_req,
+                           void* stream);
+
+/*
+ * The attention weight that every cached row receives in one layer, summed over
+ * the queries that see it (the visibility of recache_attend_cached):
+ *   res_w[g][row] = res_w_prior[g][row] + sum over requests b that list the
+ *       row's resource r (if route_mask[r][layer][g]), query heads h of g and
+ *       queries i of exp(softmax_scale q[b, i, h] . res_k[g][row] - lse[h][b, i])
+ *   ctx_w[g][row] = ctx_w_prior[g][row] + the same over the queries of the row's
+ *       request that see it (causal, bottom-right aligned).
+ * Priors may be NULL (zeros) or the output arrays themselves (accumulation in
+ * place, over layers or steps).  Sums are fp32 and made in one order: the same
+ * call gives the same bits.
+ *   q[total_q][n_q_heads][head_dim]: rotated queries; lse[n_q_heads][total_q]:
+ *       what recache_attend_cached wrote for them
+ *   cu_q, cu_ctx: as there, 1 <= Tq_b <= Tc_b; max_q >= every Tq_b; with max_q
+ *       = 1 every request must have exactly one query (NaN weights for one that
+ *       has not)
+ *   ctx_k[n_kv_heads][ctx_rows][head_dim], ctx_w (_prior)[n_kv_heads][ctx_rows];
+ *       ctx_w NULL: contexts are not weighed
+ *   res_k: [n_kv_heads][res_rows][head_dim] with res_w (_prior)[n_kv_heads]
+ *       [res_rows], rows cu_kept[r] .. cu_kept[r+1); or with res_off (this
+ *       layer's row of recache_route_store_offsets' table) a route-compacted
+ *       store [res_rows][head_dim] with [res_rows] weights; res_w NULL: resources
+ *       are not weighed
+ *   route_mask[n_res][n_layers][n_kv_heads]; user_off, user_req: of
+ *       recache_resource_users, n_users entries
+ * Rows of invisible routes get their prior (0 without one); rows of no segment
+ * are left as they are.
+ * Errors: RECACHE_EINVAL, and RECACHE_EUNSUPPORTED for dtype / head_dim / more
+ * than 8 query heads per KV head in bf16.
+ */
+int recache_attend_weights(int dtype, int layer, int n_layers, int n_req, const int32_t* cu_q,
+                           const int32_t* cu_ctx, int total_q, int max_q, int n_q_heads,
+                           int n_kv_heads, int head_dim, float softmax_scale, const void* q,
+                           const float* lse, const void* ctx_k, int ctx_rows,
+                           const float* ctx_w_prior, float* ctx_w, const void* res_k, int res_rows,
+                           const float* res_w_prior, float* res_w, int n_res,
+                           const int32_t* cu_kept, const int32_t* res_off,
+                           const uint8_t* route_mask, const int32_t* user_off,
+                           const int32_t* user_req, int n_users, void* stream);
+
+/*
+ * Kept lists by score: of every segment s (a resource, or a request's context)
+ * with rows [cu[s], cu[s+1]) the cu_kept[s+1] - cu_kept[s] best rows stay, in
+ * ascending order of their local indices:
+ *   kept_idx[cu_kept[s] .. cu_kept[s+1]), as recache_prune_gather takes them.
+ * A row's score is the sum of its weights over the planes (KV heads, or KV heads
+ * of several layers), formed in 64 bits and rounded to 32; equal scores go to
+ * the lower index, and NaN is below every number.  The last keep_last rows of a
+ * segment stay whatever they score (the newest tokens; a resource's suffix), and
+ * the first keep_first (as many of both as the segment keeps, the last ones
+ * first).
+ *   cu[n_seg + 1] from 0 to total, cu_kept[n_seg + 1] from 0 to total_kept
+ *       (device int32), 0 <= cu_kept[s+1] - cu_kept[s] <= cu[s+1] - cu[s]
+ *   max_len: at least the longest segment (a longer one keeps no rows:
+ *       its kept_idx are -1, its kept weights NaN)
+ *   w[n_planes][total] fp32; kept_w[n_planes][total_kept] or NULL: the kept
+ *       rows' weights, from which accumulation goes on over the pruned cache
+ *   workspace: device scratch of recache_select_workspace_bytes(...) bytes
+ *       (may be NULL when that is 0); contents need no initialisation
+ * Errors: RECACHE_EINVAL for bad sizes or null pointers, RECACHE_EWORKSPACE.
+ */
+size_t recache_select_workspace_bytes(int n_seg, int total, int max_len);
+int recache_select_kept(int n_seg, const int32_t* cu, int total, int max_len, int n_planes,
+                        const float* w, const int32_t* cu_kept, int total_kept, int keep_first,
+                        int keep_last, int32_t* kept_idx, float* kept_w, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/*
+ * 8-bit caches (library convention): e4m3 codes (OCP: 4 exponent and 3 mantissa
+ * bits, largest value 448, no infinities) in the layouts of the bf16 caches, one
+ * byte per element, and for every RECACHE_BLOCK_TOKENS tokens of a segment and
+ * plane one scale 2^(e - 127), held as the byte e.  The value of a code is
+ * code * 2^(e - 127), exact in bf16.  A segment is what attention reads as one
+ * run of rows: a resource of a cache (cu = cu_kept), a route (r, g) of a store
+ * (number r * n_kv_heads + g, cu = the store's row table), a request's context.
+ * The scale of token j of segment s is byte cu[s] / RECACHE_BLOCK_TOKENS + s +
+ * j / RECACHE_BLOCK_TOKENS of its plane, which has recache_quantized_blocks(rows,
+ * n_seg) = rows / RECACHE_BLOCK_TOKENS + n_seg bytes (some of them unused).
+ *
+ * recache_quantize_kv writes K and V rows (which keep their own scales) of
+ * every segment and plane.  Segment s has len[s] rows in the cache from row
+ * cu[s] on (len NULL: cu[s+1] - cu[s]; a segment may have room for more), the
+ * last cu_new[s+1] - cu_new[s] of which are new and come from the source rows
+ * [cu_new[s], cu_new[s+1]) (cu_new NULL: all of them, from the rows of the same
+ * numbers).  For each block of 64 tokens:
+ *   e = the smallest e >= 1 with |x| <= 448 * 2^(e - 127) for every finite x
+ *       of the block's new rows, and at least the e that rows already there have
+ *   code = round-to-nearest-even of x * 2^(127 - e); NaN for x not finite
+ * Where e grows, the codes already there are rounded again to the new scale
+ * (exact but for those that become subnormal), so that appending tokens one by
+ * one can differ from writing them together.
+ *   k, v: source element (plane p, row t, dim i) at p * plane_stride + t *
+ *       row_stride + i (elements): a head-major cache (head_dim, rows * head_dim),
+ *       a projection [rows][n_kv_heads][head_dim] (n_kv_heads * head_dim,
+ *       head_dim), ...; 16-byte aligned, strides multiples of 16 bytes
+ *   src_rows: rows of a plane of the source (those that cu_new or cu names)
+ *   k8, v8[n_planes][rows][head_dim]; k_exp, v_exp[n_planes][blocks]
+ * Rows and scales that no new row touches are left as they are.
+ * Errors: RECACHE_EINVAL, RECACHE_EUNSUPPORTED for dtype / head_dim.
+ */
+#define RECACHE_BLOCK_TOKENS 64
+size_t recache_quantized_blocks(int rows, int n_seg);
+int recache_quantize_kv(int dtype, int n_seg, const int32_t* cu, const int32_t* len, int rows,
+                        int n_planes, int head_dim, const int32_t* cu_new, int src_rows,
+                        const void* k, const void* v, int64_t row_stride, int64_t plane_stride,
+                        uint8_t* k8, uint8_t* v8, uint8_t* k_exp, uint8_t* v_exp, void* stream);
+
+/*
+ * recache_attend_cached over 8-bit caches, resource rows and context alike
+ * (bf16 queries and outputs).  The result is that of the call on the caches'
+ * values in bf16, up to the order of the sums.  Beside its arguments:
+ *   ctx_k/ctx_v, ctx_k_exp/ctx_v_exp: planes of ctx_rows rows, segments cu_ctx
+ *   ctx_len[n_req] (device int32) or NULL: context rows in use, Tc_b =
+ *       ctx_len[b] <= cu_ctx[b+1] - cu_ctx[b], so that contexts grow in place;
+ *       max_ctx >= every Tc_b
+ *   res_k/res_v, res_k_exp/res_v_exp: planes of res_rows rows, segments cu_kept
+ *       (n_res of them), or with res_off one plane of res_rows rows, segments
+ *       res_off (n_res * n_kv_heads)
+ * The workspace is that of recache_attend_workspace_bytes.  A KV plane may be
+ * of any size.
+ * Errors: those of recache_attend_cached; RECACHE_EUNSUPPORTED for dtype
+ * RECACHE_F32.
+ */
+int recache_attend_quantized(int dtype, int layer, int n_layers, int n_req, const int32_t* cu_q,
+                             const int32_t* cu_ctx, const int32_t* ctx_len, int total_q, int max_q,
+                             int max_ctx, int max_kv, int max_route_len, int n_q_heads,
+                             int n_kv_heads, int head_dim, float softmax_scale, const void* q,
+                             const uint8_t* ctx_k, const uint8_t* ctx_v, const uint8_t* ctx_k_exp,
+                             const uint8_t* ctx_v_exp, int ctx_rows, const uint8_t* res_k,
+                             const uint8_t* res_v, const uint8_t* res_k_exp,
+                             const uint8_t* res_v_exp, int res_rows, int n_res,
+                             const int32_t* cu_kept, const int32_t* res_off,
+                             const int32_t* route_off, const int32_t* route_res,
+                             const int32_t* route_tokens, const int32_t* plan, void* out,
+                             float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * [host] Validators for host copies of index arrays.  The device kernels trust

@@ -16,6 +16,7 @@
 
 #include "recache.h"
 #include "kernels.hpp"
+#include "quant8.hpp"
 
 using namespace rc;
 
@@ -716,6 +717,281 @@ int recache_check_requests(const int32_t* req_res_off, const int32_t* req_res, i
         REQUIRE(req_res[j] >= 0 && req_res[j] < n_res, RECACHE_EINVAL,
                 "req_res[%d] = %d outside [0, %d)", j, req_res[j], n_res);
     return ok();
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// Eviction by accumulated attention weight, and 8-bit caches.
+
+extern "C" {
+
+int recache_resource_users(int n_req, const int32_t* req_res_off, const int32_t* req_res,
+                           int total_req_res, int n_res, int32_t* user_off, int32_t* user_req,
+                           void* stream) {
+    REQUIRE(n_req >= 1 && n_res >= 1 && total_req_res >= 0, RECACHE_EINVAL,
+            "n_req %d / n_res %d must be >= 1, total_req_res %d >= 0", n_req, n_res, total_req_res);
+    REQUIRE(req_res_off && user_off && (total_req_res == 0 || (req_res && user_req)), RECACHE_EINVAL,
+            "null pointer argument");
+    (void)hipGetLastError();
+    return hip_status(launch_resource_users(n_req, req_res_off, req_res, total_req_res, n_res, user_off,
+                                            user_req, as_stream(stream)),
+                      "recache_resource_users launch");
+}
+
+int recache_attend_weights(int dtype, int layer, int n_layers, int n_req, const int32_t* cu_q,
+                           const int32_t* cu_ctx, int total_q, int max_q, int n_q_heads,
+                           int n_kv_heads, int head_dim, float softmax_scale, const void* q,
+                           const float* lse, const void* ctx_k, int ctx_rows,
+                           const float* ctx_w_prior, float* ctx_w, const void* res_k, int res_rows,
+                           const float* res_w_prior, float* res_w, int n_res,
+                           const int32_t* cu_kept, const int32_t* res_off,
+                           const uint8_t* route_mask, const int32_t* user_off,
+                           const int32_t* user_req, int n_users, void* stream) {
+    int rc_ = check_dtype_dim(dtype, head_dim);
+    if (rc_) return rc_;
+    if ((rc_ = check_heads(dtype, n_q_heads, n_kv_heads))) return rc_;
+    REQUIRE(n_layers >= 1 && layer >= 0 && layer < n_layers, RECACHE_EINVAL, "layer %d outside [0, %d)", layer,
+            n_layers);
+    REQUIRE(n_req >= 1 && max_q >= 1, RECACHE_EINVAL, "n_req %d / max_q %d must be >= 1", n_req, max_q);
+    REQUIRE(total_q >= n_req && (long)total_q <= (long)n_req * max_q, RECACHE_EINVAL,
+            "total_q %d outside [n_req, n_req * max_q] = [%d, %ld]", total_q, n_req, (long)n_req * max_q);
+    REQUIRE(!(isnan(softmax_scale) || isinf(softmax_scale)), RECACHE_EINVAL, "softmax_scale not finite");
+    REQUIRE(ctx_w || res_w, RECACHE_EINVAL, "neither ctx_w nor res_w");
+    REQUIRE((((uintptr_t)q | (uintptr_t)(ctx_w ? ctx_k : nullptr) | (uintptr_t)(res_w ? res_k : nullptr)) & 15) == 0,
+            RECACHE_EINVAL, "q, ctx_k and res_k must be 16-byte aligned");
+    REQUIRE(q && lse && cu_q && cu_ctx, RECACHE_EINVAL, "null pointer argument");
+    REQUIRE(!ctx_w || (ctx_k && ctx_rows >= 1), RECACHE_EINVAL, "ctx_w needs ctx_k and ctx_rows >= 1 (%d)", ctx_rows);
+    REQUIRE(!res_w || (n_res >= 1 && cu_kept && route_mask && user_off && n_users >= 0 && (n_users == 0 || user_req)),
+            RECACHE_EINVAL, "res_w needs cu_kept, route_mask, user_off and user_req (n_res %d, n_users %d)", n_res,
+            n_users);
+    // a route-compacted store may hold no rows for a layer outside every route
+    REQUIRE(!res_w || res_rows >= (res_off ? 0 : 1), RECACHE_EINVAL, "res_rows %d too small", res_rows);
+    REQUIRE(!res_w || res_k || res_rows == 0, RECACHE_EINVAL, "res_w needs res_k");
+    WeighArgs a{};
+    a.n_req = n_req;
+    a.n_res = n_res;
+    a.n_q_heads = n_q_heads;
+    a.n_kv_heads = n_kv_heads;
+    a.ratio = n_q_heads / n_kv_heads;
+    a.one_query = max_q == 1;
+    a.scale_log2 = resolve_scale(softmax_scale, head_dim) * 1.4426950408889634f;
+    a.q = q;
+    a.lse = lse;
+    a.total_q = total_q;
+    a.cu_q = cu_q;
+    a.cu_ctx = cu_ctx;
+    a.ck = ctx_k;
+    a.c_rows = ctx_rows;
+    a.c_prior = ctx_w_prior;
+    a.c_w = ctx_w;
+    a.rk = res_k;
+    a.r_rows = res_rows;
+    a.r_prior = res_w_prior;
+    a.r_w = res_rows > 0 ? res_w : nullptr;
+    a.cu_kept = cu_kept;
+    a.res_off = res_off;
+    a.mask = route_mask;
+    a.layer = layer;
+    a.n_layers = n_layers;
+    a.user_off = user_off;
+    a.user_req = user_req;
+    a.n_users = n_users;
+    (void)hipGetLastError();
+    return hip_status(launch_weigh(a, dtype == RECACHE_F32 ? 4 : 2, head_dim, as_stream(stream)),
+                      "recache_attend_weights launch");
+}
+
+size_t recache_select_workspace_bytes(int n_seg, int total, int max_len) {
+    if (n_seg < 1 || total < 0 || max_len < 0) return 0;
+    return select_workspace_bytes(total, max_len);
+}
+
+int recache_select_kept(int n_seg, const int32_t* cu, int total, int max_len, int n_planes,
+                        const float* w, const int32_t* cu_kept, int total_kept, int keep_first,
+                        int keep_last, int32_t* kept_idx, float* kept_w, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+    REQUIRE(n_seg >= 1 && n_planes >= 1, RECACHE_EINVAL, "n_seg %d / n_planes %d must be >= 1", n_seg, n_planes);
+    REQUIRE(total >= 0 && total_kept >= 0 && total_kept <= total, RECACHE_EINVAL,
+            "total_kept %d outside [0, total] = [0, %d]", total_kept, total);
+    REQUIRE(max_len >= 0 && max_len <= total, RECACHE_EINVAL, "max_len %d outside [0, %d]", max_len, total);
+    REQUIRE(keep_first >= 0 && keep_last >= 0, RECACHE_EINVAL, "keep_first %d / keep_last %d must be >= 0",
+            keep_first, keep_last);
+    REQUIRE(cu && cu_kept && (total == 0 || w) && (total_kept == 0 || kept_idx), RECACHE_EINVAL,
+            "null pointer argument");
+    const size_t need = select_workspace_bytes(total, max_len);
+    REQUIRE(need == 0 || (workspace && workspace_bytes >= need), RECACHE_EWORKSPACE,
+            "selection from segments of %d rows needs a %zu-byte workspace, got %zu", max_len, need,
+            workspace ? workspace_bytes : 0);
+    REQUIRE(((uintptr_t)workspace & 3) == 0, RECACHE_EINVAL, "workspace is not 4-byte aligned");
+    if (total_kept == 0) return ok();
+    SelectArgs a{};
+    a.n_seg = n_seg;
+    a.n_planes = n_planes;
+    a.cu = cu;
+    a.total = total;
+    a.w = w;
+    a.cu_kept = cu_kept;
+    a.total_kept = total_kept;
+    a.keep_first = keep_first;
+    a.keep_last = keep_last;
+    a.kept_idx = kept_idx;
+    a.kept_w = kept_w;
+    a.max_len = max_len;
+    a.keys = static_cast<uint32_t*>(workspace);
+    (void)hipGetLastError();
+    return hip_status(launch_select(a, as_stream(stream)), "recache_select_kept launch");
+}
+
+size_t recache_quantized_blocks(int rows, int n_seg) {
+    if (rows < 0 || n_seg < 0) return 0;
+    return (size_t)block_slots(rows, n_seg);
+}
+
+int recache_quantize_kv(int dtype, int n_seg, const int32_t* cu, const int32_t* len, int rows,
+                        int n_planes, int head_dim, const int32_t* cu_new, int src_rows,
+                        const void* k, const void* v, int64_t row_stride, int64_t plane_stride,
+                        uint8_t* k8, uint8_t* v8, uint8_t* k_exp, uint8_t* v_exp, void* stream) {
+    int rc_ = check_dtype_dim(dtype, head_dim);
+    if (rc_) return rc_;
+    REQUIRE(n_seg >= 1 && n_planes >= 1, RECACHE_EINVAL, "n_seg %d / n_planes %d must be >= 1", n_seg, n_planes);
+    REQUIRE(rows >= 0 && src_rows >= 0, RECACHE_EINVAL, "rows %d / src_rows %d must be >= 0", rows, src_rows);
+    REQUIRE(cu, RECACHE_EINVAL, "null pointer argument");
+    if (rows == 0 || src_rows == 0) return ok();
+    REQUIRE(k && v && k8 && v8 && k_exp && v_exp, RECACHE_EINVAL, "null pointer argument");
+    const int per16 = dtype == RECACHE_F32 ? 4 : 8;
+    REQUIRE(row_stride >= 0 && plane_stride >= 0 && row_stride % per16 == 0 && plane_stride % per16 == 0,
+            RECACHE_EINVAL, "strides %lld, %lld (rows, planes) must be non-negative multiples of 16 bytes",
+            (long long)row_stride, (long long)plane_stride);
+    REQUIRE(((uintptr_t)k & 15) == 0 && ((uintptr_t)v & 15) == 0 && ((uintptr_t)k8 & 15) == 0 &&
+                ((uintptr_t)v8 & 15) == 0,
+            RECACHE_EINVAL, "k, v, k8 and v8 must be 16-byte aligned");
+    QuantizeArgs a{};
+    a.n_seg = n_seg;
+    a.n_planes = n_planes;
+    a.cu = cu;
+    a.len = len;
+    a.cu_new = cu_new;
+    a.rows = rows;
+    a.n_slots = block_slots(rows, n_seg);
+    a.src_rows = src_rows;
+    a.n_blocks = (cu_new ? src_rows : rows) / kBlk8 + (cu_new ? 2L : 1L) * n_seg;
+    a.k = k;
+    a.v = v;
+    a.row_stride = row_stride;
+    a.plane_stride = plane_stride;
+    a.k8 = k8;
+    a.v8 = v8;
+    a.k_exp = k_exp;
+    a.v_exp = v_exp;
+    (void)hipGetLastError();
+    return hip_status(launch_quantize(a, dtype == RECACHE_F32 ? 4 : 2, head_dim, as_stream(stream)),
+                      "recache_quantize_kv launch");
+}
+
+int recache_attend_quantized(int dtype, int layer, int n_layers, int n_req, const int32_t* cu_q,
+                             const int32_t* cu_ctx, const int32_t* ctx_len, int total_q, int max_q,
+                             int max_ctx, int max_kv, int max_route_len, int n_q_heads,
+                             int n_kv_heads, int head_dim, float softmax_scale, const void* q,
+                             const uint8_t* ctx_k, const uint8_t* ctx_v, const uint8_t* ctx_k_exp,
+                             const uint8_t* ctx_v_exp, int ctx_rows, const uint8_t* res_k,
+                             const uint8_t* res_v, const uint8_t* res_k_exp,
+                             const uint8_t* res_v_exp, int res_rows, int n_res,
+                             const int32_t* cu_kept, const int32_t* res_off,
+                             const int32_t* route_off, const int32_t* route_res,
+                             const int32_t* route_tokens, const int32_t* plan, void* out,
+                             float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    REQUIRE(((uintptr_t)plan & 3) == 0, RECACHE_EINVAL, "plan is not 4-byte aligned");
+    // (planes of 8 bits have no size limit, so the check is told of small ones)
+    int rc_ = check_attend(dtype, layer, n_layers, n_req, cu_q, cu_ctx, total_q, max_q, max_ctx,
+                           max_route_len, n_q_heads, n_kv_heads, head_dim, softmax_scale, q, ctx_k,
+                           ctx_v, std::min(ctx_rows, 1), res_k, res_v, std::min(res_rows, 1), cu_kept, res_off,
+                           route_off, route_res, route_tokens, out);
+    if (rc_) return rc_;
+    REQUIRE(dtype == RECACHE_BF16, RECACHE_EUNSUPPORTED, "8-bit caches are attended in bf16 only");
+    REQUIRE(n_res >= 1, RECACHE_EINVAL, "n_res %d must be >= 1", n_res);
+    REQUIRE(ctx_k_exp && ctx_v_exp && ((res_k_exp && res_v_exp) || res_rows == 0), RECACHE_EINVAL,
+            "null scale pointer");
+    REQUIRE((((uintptr_t)q | (uintptr_t)out | (uintptr_t)ctx_k | (uintptr_t)ctx_v | (uintptr_t)res_k |
+              (uintptr_t)res_v) & 15) == 0,
+            RECACHE_EINVAL, "q, out and the caches must be 16-byte aligned");
+    Cache8 c{};
+    c.rk = res_k;
+    c.rv = res_v;
+    c.rk_exp = res_k_exp;
+    c.rv_exp = res_v_exp;
+    c.r_slots = block_slots(res_rows, res_off ? (long)n_res * n_kv_heads : n_res);
+    c.r_sstride = res_off ? 0 : c.r_slots;
+    c.ck = ctx_k;
+    c.cv = ctx_v;
+    c.ck_exp = ctx_k_exp;
+    c.cv_exp = ctx_v_exp;
+    c.c_slots = block_slots(ctx_rows, n_req);
+    c.ctx_len = ctx_len;
+    const float scale_log2 = resolve_scale(softmax_scale, head_dim) * 1.4426950408889634f;
+    const hipStream_t s = as_stream(stream);
+    (void)hipGetLastError();
+    if (max_q == 1) {
+        const int n_splits = decode_splits(n_req, n_kv_heads, max_kv > 0 ? max_kv : max_ctx);
+        const size_t need = decode_workspace_bytes((long)n_req * n_splits, n_q_heads, head_dim);
+        REQUIRE(workspace && workspace_bytes >= need, RECACHE_EWORKSPACE,
+                "decode needs a %zu-byte workspace, got %zu", need, workspace ? workspace_bytes : 0);
+        Decode8Args a{};
+        static_cast<Cache8&>(a) = c;
+        a.d.n_req = n_req;
+        a.d.n_q_heads = n_q_heads;
+        a.d.n_kv_heads = n_kv_heads;
+        a.d.ratio = n_q_heads / n_kv_heads;
+        a.d.head_dim = head_dim;
+        a.d.n_splits = n_splits;
+        a.d.scale_log2 = scale_log2;
+        a.d.q = static_cast<const uint16_t*>(q);
+        a.d.out = static_cast<uint16_t*>(out);
+        a.d.lse = lse;
+        a.d.lse_rows = total_q;
+        a.d.r_rows = res_rows;
+        a.d.r_gstride = res_off ? 0 : res_rows;
+        a.d.res_off = res_off;
+        a.d.c_rows = ctx_rows;
+        a.d.max_ctx_rows = (long)n_req * max_ctx;
+        a.d.cu_q = cu_q;
+        a.d.cu_ctx = cu_ctx;
+        a.d.layer = layer;
+        a.d.n_layers = n_layers;
+        a.d.route_off = route_off;
+        a.d.route_res = route_res;
+        a.d.cu_kept = cu_kept;
+        a.d.ws_o = static_cast<float*>(workspace);
+        a.d.ws_ml = a.d.ws_o + (size_t)n_req * n_q_heads * n_splits * head_dim;
+        a.d.plan = plan;
+        return hip_status(launch_decode8(a, s), "attend (8-bit decode) launch");
+    }
+    Attn8Args a{};
+    static_cast<Cache8&>(a) = c;
+    a.a.n_q_heads = n_q_heads;
+    a.a.n_kv_heads = n_kv_heads;
+    a.a.ratio = n_q_heads / n_kv_heads;
+    a.a.max_rows = max_q;
+    a.a.n_units = n_req;
+    a.a.scale_log2 = scale_log2;
+    a.a.q = static_cast<const uint16_t*>(q);
+    a.a.out = static_cast<uint16_t*>(out);
+    a.a.lse = lse;
+    a.a.lse_rows = total_q;
+    a.a.k_rows = res_rows;
+    a.a.k_gstride = res_off ? 0 : res_rows;
+    a.a.res_off = res_off;
+    a.a.cu_q = cu_q;
+    a.a.cu_ctx = cu_ctx;
+    a.a.c_rows = ctx_rows;
+    a.a.layer = layer;
+    a.a.n_layers = n_layers;
+    a.a.route_off = route_off;
+    a.a.route_res = route_res;
+    a.a.cu_kept = cu_kept;
+    a.a.plan = plan;
+    a.a.max_keys = max_kv;
+    return hip_status(launch_attn8(a, head_dim, s), "attend (8-bit prefill) launch");
 }
 
 }  // extern "C"

@@ -1,0 +1,428 @@
+// Conversation prefill over caches in 8 bits (quant8.hpp), keys split over a
+// block's waves: the decomposition of attn_split.hip, on e4m3 rows.
+//
+// As in decode8.hip a tile lies in one scale block (here 32 of its 64 rows),
+// so that its rows are one run of memory and its two scales are operands of the
+// conversions.  Codes go into LDS as they are and become bf16 as the MFMA
+// fragments are read: K 16 dims per 16-byte read, V by 8-bit transpose reads
+// (eight keys of one dim per lane).  At half the bytes both buffers of a wave
+// fit twice, and the next tile's copies are in flight for the whole of a tile.
+#include <algorithm>
+
+#include "attn_split.hpp"
+#include "attn_tile.hpp"
+#include "common.hpp"
+#include "kernels.hpp"
+#include "quant8.hpp"
+
+namespace rc {
+
+namespace {
+
+constexpr int kKeys = 32;  // keys per wave tile
+typedef int v2i __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) v2i lds_v2i;
+
+template <int C>
+struct Tag {
+    static constexpr int value = C;
+};
+
+// Segments of a stream in tiles: segment i has tiles [end[i - 1], end[i]).  The
+// merge's (max, sum) take the same memory after the loop.
+template <int W>
+union Split8Smem {
+    struct {
+        int end[kMaxSeg];
+        int row[kMaxSeg];  // first row
+        int len[kMaxSeg];  // rows
+        int id[kMaxSeg];   // number in its cache, of the scale slots
+    } seg;
+    float ml[W][kCols][2];
+};
+
+// Chunk swizzles of tile rows.  K: 16 consecutive rows of one chunk fall on
+// distinct banks; V: the 8 rows x 2 chunks that half a wave's transpose read
+// touches.
+template <int HD>
+__device__ __forceinline__ int k_mask8(int row) {
+    return HD == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
+}
+template <int HD>
+__device__ __forceinline__ int vt_mask8(int row) {
+    return HD == 128 ? (((row >> 1) & 1) << 1) | (((row >> 3) & 1) << 2) : ((row >> 3) & 1) << 1;
+}
+
+template <int HD, int W, bool COMPACT>
+__global__ __launch_bounds__(W * 64, 2) void attn_split8_kernel(const Attn8Args x) {
+    const AttnArgs& a = x.a;
+    constexpr int kThreads = W * 64;
+    constexpr int CPR = HD / 16;       // 16-byte chunks per row
+    constexpr int NT = HD / 16;        // MFMA k-steps over head_dim
+    constexpr int NC = HD / 32;        // 16-byte K reads per lane (two steps each)
+    constexpr int NDB = HD / 32;       // 32-wide blocks of head_dim
+    constexpr int RPI = 64 / CPR;      // rows per 1 KB wave copy
+    constexpr int NJ = kKeys / RPI;    // copies per K or V tile
+    constexpr int TILEB = kKeys * HD;
+    constexpr int NLOAD = 2 * NJ + 1;  // vector memory operations per tile
+    constexpr int WAIT_PREV = (NLOAD & 15) | ((NLOAD >> 4) << 14) | 0x0F70;
+    __shared__ Split8Smem<W> sm;
+    // Per wave two stages of a K and a V tile, in two arrays: the compiler then
+    // sees that copies in flight into one do not touch the other.  Before the
+    // loop the first holds the scan of the segment lengths; after it the two
+    // hold the lower and upper dims of the wave's O, fp32 [32 columns][HD / 2].
+    __shared__ __attribute__((aligned(16))) char st0[W][2 * TILEB], st1[W][2 * TILEB];
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, half = lane >> 5;
+    const int R = a.ratio;
+
+    // block -> (unit, column block [longest first], group), as in attn_split.hip
+    int bid = blockIdx.x;
+    int g = bid % a.n_kv_heads;
+    bid /= a.n_kv_heads;
+    int cb, unit;
+    if constexpr (COMPACT) {
+        const int2 at = nth_col_block(a, bid, lane);
+        unit = at.x, cb = at.y;
+        if (unit < 0) return;  // the grid is a bound on the blocks there are
+        g = (g + unit) % a.n_kv_heads;
+    } else {
+        cb = a.n_qt - 1 - bid % a.n_qt;
+        unit = bid / a.n_qt;
+        if (a.plan) {
+            const int n_pairs = a.n_units * a.n_kv_heads;
+            int p = a.plan[(size_t)a.layer * n_pairs + unit * a.n_kv_heads + g];
+            p = min(max(p, 0), n_pairs - 1);  // in bounds whatever the plan holds
+            unit = p / a.n_kv_heads;
+            g = p % a.n_kv_heads;
+        } else {
+            g = (g + unit) % a.n_kv_heads;
+        }
+    }
+    const int q_row0 = a.cu_q[unit], q_len = a.cu_q[unit + 1] - q_row0;
+    const int c0 = __builtin_amdgcn_readfirstlane(a.cu_ctx[unit]);
+    const int tc = __builtin_amdgcn_readfirstlane(x.ctx_len ? x.ctx_len[unit] : a.cu_ctx[unit + 1] - c0);
+    // the grid covers max_rows rows; the last block answers for any beyond
+    if (cb == a.n_qt - 1 && q_len > a.max_rows)
+        poison_rows<HD>(a, g * R, R, q_row0, a.max_rows, q_len, tid, kThreads);
+    const int j0 = cb * kCols, n_cols = min(q_len, a.max_rows) * R;
+    if (j0 >= n_cols) return;
+    const int used = min(kCols, n_cols - j0);
+    const int my_j = j0 + min(l32, used - 1);  // spare lanes repeat the last column
+    const int my_row = my_j / R, my_head = g * R + my_j % R;
+    const int first_row = j0 / R, last_row = (j0 + used - 1) / R;
+
+    // ---- Q^T (B operand) in K's order of dims: step t holds dims
+    // (t / 2) * 32 + half * 16 + (t % 2) * 8 + [0, 8) of this lane's column
+    bf16x8 qf[NT];
+    {
+        const long row = max(0L, min((long)q_row0 + my_row, a.lse_rows - 1));
+        const uint16_t* qp = a.q + ((size_t)row * a.n_q_heads + my_head) * HD + half * 16;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+            qf[t] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qp + (t >> 1) * 32 + (t & 1) * 8));
+    }
+
+    // ---- visible segments of this (request, layer, group), in tiles
+    const size_t e = ((size_t)unit * a.n_layers + a.layer) * a.n_kv_heads + g;
+    const int r0 = a.route_off[e];
+    const int n_seg = a.route_off[e + 1] - r0;
+    if (n_seg > kMaxSeg) {
+        for (int j = j0 + wave; j < j0 + used; j += W)
+            poison_rows<HD>(a, g * R + j % R, 1, q_row0, j / R, j / R + 1, lane, 64);
+        return;
+    }
+    int n_segt = 0;
+    {
+        int* scan = reinterpret_cast<int*>(st0[0]);
+        for (int s0 = 0, k = 0; s0 < n_seg; s0 += kThreads, k ^= 1) {
+            const int s = s0 + tid;
+            int tiles = 0;
+            if (s < n_seg) {
+                const int r = a.route_res[r0 + s];
+                const int k0 = a.cu_kept[r];
+                const int id = a.res_off ? r * a.n_kv_heads + g : r;
+                const int len = max(a.cu_kept[r + 1] - k0, 0);
+                sm.seg.row[s] = a.res_off ? a.res_off[id] : k0;
+                sm.seg.len[s] = len;
+                sm.seg.id[s] = id;
+                tiles = (len + kKeys - 1) / kKeys;
+            }
+            int total;
+            const int at = n_segt + block_exclusive_scan<W>(tiles, scan + k * W, &total);
+            if (s < n_seg) sm.seg.end[s] = at + tiles;
+            n_segt += total;
+        }
+        __syncthreads();
+        n_segt = __builtin_amdgcn_readfirstlane(n_segt);
+    }
+    const int off = tc - q_len;                          // a column sees causal rows <= off + row
+    const int n_ctx = max(0, min(off + last_row + 1, tc));  // causal rows the block sees
+    const int n_tiles = n_segt + (n_ctx + kKeys - 1) / kKeys;
+
+    // ---- HBM -> LDS copies of one tile: rows j*RPI + [0, RPI) by copy j; lane i
+    // lands at byte 16 i of them, chunk i % CPR, which holds logical chunk
+    // (i % CPR) ^ mask(row).  The buffer resource's extent is the tile: rows
+    // past its end are zeros.
+    const int cp_row = lane / CPR;
+    int k_lane[NJ], v_lane[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+        const int row = j * RPI + cp_row;
+        k_lane[j] = row * HD + (((lane % CPR) ^ k_mask8<HD>(row)) << 4);
+        v_lane[j] = row * HD + (((lane % CPR) ^ vt_mask8<HD>(row)) << 4);
+    }
+    int exps[2], n_in[2];
+    int u_i = 0, u_lo = 0;  // wave-uniform walk over the segments: the current one, its first tile
+    auto uniform = [](uint64_t u) {
+        return ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32) |
+               (uint32_t)__builtin_amdgcn_readfirstlane((int)u);
+    };
+    auto load_tile = [&](auto buf_tag, int t) {
+        constexpr int buf = decltype(buf_tag)::value;
+        const bool seg = t < n_segt;
+        long row, slot, rows;
+        int n;
+        if (seg) {
+            int hi = __builtin_amdgcn_readfirstlane(sm.seg.end[u_i]);
+            while (t >= hi && u_i + 1 < n_seg) {
+                ++u_i;
+                u_lo = hi;
+                hi = __builtin_amdgcn_readfirstlane(sm.seg.end[u_i]);
+            }
+            const int j = t - u_lo, beg = __builtin_amdgcn_readfirstlane(sm.seg.row[u_i]);
+            row = (long)beg + (long)j * kKeys;
+            slot = block_slot(beg, __builtin_amdgcn_readfirstlane(sm.seg.id[u_i])) + j * kKeys / kBlk8;
+            n = __builtin_amdgcn_readfirstlane(sm.seg.len[u_i]) - j * kKeys;
+            rows = a.k_rows;
+            slot = max(0L, min(slot, x.r_slots - 1));
+        } else {
+            const int j = t - n_segt;
+            row = (long)c0 + (long)j * kKeys;
+            slot = block_slot(c0, unit) + j * kKeys / kBlk8;
+            n = n_ctx - j * kKeys;
+            rows = a.c_rows;
+            slot = max(0L, min(slot, x.c_slots - 1));
+        }
+        // in bounds whatever the tables hold: the tile's extent ends at the plane's
+        row = max(0L, min(row, rows - 1));
+        n = (int)max(0L, min((long)min(n, kKeys), rows - row));
+        n_in[buf] = n;
+        const size_t base = ((size_t)g * (seg ? a.k_gstride : a.c_rows) + row) * HD;
+        const int bytes = __builtin_amdgcn_readfirstlane(n * HD);
+        const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(
+            (void*)uniform((uint64_t)((seg ? x.rk : x.ck) + base)), (short)0, bytes, kBufferFlags);
+        const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(
+            (void*)uniform((uint64_t)((seg ? x.rv : x.cv) + base)), (short)0, bytes, kBufferFlags);
+        const size_t at = (size_t)g * (seg ? x.r_sstride : x.c_slots) + slot;
+        exps[buf] = lane < 32 ? (seg ? x.rk_exp : x.ck_exp)[at] : (seg ? x.rv_exp : x.cv_exp)[at];
+        char* dst = buf ? st1[wave] : st0[wave];
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_void*)(dst + j * 1024), 16, (int)k_lane[j], 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_void*)(dst + TILEB + j * 1024), 16, (int)v_lane[j], 0, 0, 0);
+    };
+
+    // K as the A operand: key l32, chunk 2c + half
+    const uint32_t k_rd0 = (uint32_t)(l32 * HD + ((half ^ k_mask8<HD>(l32)) << 4));
+    // V^T transpose reads: in a 16-lane group G, lanes 2k and 2k + 1 point at the
+    // two halves of row k's chunk, and lane i receives column i of the 8 rows:
+    // rows s*16 + w*8 + half*4 + [0, 4) (w = 0, 1), the keys that P^T holds in
+    // slots w*4 + [0, 4) of step s; dims db*32 + (G & 1)*16 + i.
+    uint32_t v_rd0;
+    {
+        const int G = lane >> 4, i = lane & 15, k = i >> 1;
+        const int row = (k >> 2) * 8 + (G >> 1) * 4 + (k & 3);
+        v_rd0 = (uint32_t)(row * HD + (((G & 1) ^ vt_mask8<HD>(row)) << 4) + (i & 1) * 8);
+    }
+
+    const float sl2 = a.scale_log2;
+    const bf16x2 ones2 = __builtin_bit_cast(bf16x2, 0x3F803F80u);  // (1.0, 1.0) in bf16
+    float m = kNoKey, lsum = 0.f;
+    f32x16 oacc[NDB];
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) oacc[db] = f32x16{};
+
+    auto compute = [&](auto buf_tag, int t) {
+        constexpr int buf = decltype(buf_tag)::value;
+        const float ksc = block_scale((uint32_t)__builtin_amdgcn_readlane(exps[buf], 0));
+        const float vsc = block_scale((uint32_t)__builtin_amdgcn_readlane(exps[buf], 32));
+        const char* kb = buf ? st1[wave] : st0[wave];
+        const char* vb = kb + TILEB;
+        f32x16 sc = {};
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const u32x4 w = *reinterpret_cast<const u32x4*>(kb + (k_rd0 ^ (uint32_t)(c << 5)));
+            sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, codes_to_bf16x8(w[0], w[1], ksc)),
+                                                         qf[2 * c], sc, 0, 0, 0);
+            sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, codes_to_bf16x8(w[2], w[3], ksc)),
+                                                         qf[2 * c + 1], sc, 0, 0, 0);
+        }
+        // key offsets that every column of the block sees, and this lane's
+        const bool seg = t < n_segt;
+        const int p0 = (t - n_segt) * kKeys;  // (causal tiles)
+        const int lim = seg ? n_in[buf] - 1 : min(off + first_row - p0, n_in[buf] - 1);
+        if (kKeys - 1 > lim) {
+            const int rem = (seg ? n_in[buf] - 1 : min(off + my_row - p0, n_in[buf] - 1)) - half * 4;
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if ((r >> 2) * 8 + (r & 3) > rem) sc[r] = -INFINITY;
+        }
+        bf16x8 pf[2];
+        float tsum;
+        auto weights = [&]() {
+            const float msl = m * sl2;
+            tsum = 0.f;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[8 * s + 2 * i], sl2, -msl));
+                    const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[8 * s + 2 * i + 1], sl2, -msl));
+                    w[i] = pack_bf16x2(p0, p1);
+                    tsum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[i]), ones2, tsum, false);
+                }
+                pf[s] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
+            }
+        };
+        auto row_max = [&]() {
+            float mt = sc[0];
+#pragma unroll
+            for (int r = 1; r < 16; ++r) mt = fmaxf(mt, sc[r]);
+            return pair_max(mt);
+        };
+        // weights against a reference max, set by the wave's first tile and
+        // moved only when one could pass 2^16 (as in attn_split.hip)
+        if (t == wave) {
+            m = row_max();
+            if (m == -INFINITY) m = kNoKey;
+        }
+        weights();
+        if (__builtin_amdgcn_ballot_w64(!(tsum <= kWeightCap)) != 0) {
+            const float m_new = fmaxf(m, row_max());
+            const float alpha = __builtin_amdgcn_exp2f((m - m_new) * sl2);
+            lsum *= alpha;
+#pragma unroll
+            for (int db = 0; db < NDB; ++db) oacc[db] *= alpha;
+            m = m_new;
+            weights();
+        }
+        lsum += tsum;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const v2i w = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                    (lds_v2i*)(vb + (v_rd0 ^ (uint32_t)(db << 5)) + s * 16 * HD));
+                oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    __builtin_bit_cast(bf16x8, codes_to_bf16x8((uint32_t)w[0], (uint32_t)w[1], vsc)), pf[s], oacc[db],
+                    0, 0, 0);
+            }
+    };
+
+    // This wave's tiles are wave, wave + W, ...; only it touches its buffers, so
+    // waiting for its own copies is enough.
+    if (wave < n_tiles) {
+        load_tile(Tag<0>{}, wave);
+        for (int t = wave;; t += 2 * W) {
+            if (t + W >= n_tiles) {
+                __builtin_amdgcn_s_waitcnt(0x0F70);
+                compute(Tag<0>{}, t);
+                break;
+            }
+            load_tile(Tag<1>{}, t + W);
+            __builtin_amdgcn_s_waitcnt(WAIT_PREV);
+            compute(Tag<0>{}, t);
+            if (t + 2 * W >= n_tiles) {
+                __builtin_amdgcn_s_waitcnt(0x0F70);
+                compute(Tag<1>{}, t + W);
+                break;
+            }
+            load_tile(Tag<0>{}, t + 2 * W);
+            __builtin_amdgcn_s_waitcnt(WAIT_PREV);
+            compute(Tag<1>{}, t + W);
+        }
+    }
+
+    // ---- merge of the waves, as in attn_split.hip
+    lsum = pair_sum(lsum);
+    constexpr int OB = HD * 2, OC = HD / 8;  // bytes and 16-byte chunks of half an O row
+    static_assert(kCols * OB == 2 * TILEB, "half of a wave's O fills a stage");
+    __syncthreads();  // (ml shares the segment table's memory)
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+            const int c = db % (NDB / 2) * 8 + r4 * 2 + half;  // 16-byte chunk of the half row
+            *reinterpret_cast<f32x4*>((db < NDB / 2 ? st0[wave] : st1[wave]) + l32 * OB + ((c ^ (l32 % OC)) << 4)) =
+                f32x4{oacc[db][r4 * 4], oacc[db][r4 * 4 + 1], oacc[db][r4 * 4 + 2], oacc[db][r4 * 4 + 3]};
+        }
+    if (half == 0) {
+        sm.ml[wave][l32][0] = m == kNoKey ? -INFINITY : m;
+        sm.ml[wave][l32][1] = lsum;
+    }
+    __syncthreads();
+    for (int i = tid; i < used * OC; i += kThreads) {
+        const int col = i / OC, c = i % OC;
+        const int j = j0 + col, row = j / R, head = g * R + j % R;
+        float mx = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < W; ++w) mx = fmaxf(mx, sm.ml[w][col][0]);
+        float num[8] = {}, den = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const float mw = sm.ml[w][col][0];
+            const float f = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mw - mx) * sl2);
+            den += f * sm.ml[w][col][1];
+            const char* o = (c < OC / 2 ? st0[w] : st1[w]) + col * OB;
+#pragma unroll
+            for (int h2 = 0; h2 < 2; ++h2) {
+                const f32x4 v = *reinterpret_cast<const f32x4*>(o + (((c % (OC / 2) * 2 + h2) ^ (col % OC)) << 4));
+#pragma unroll
+                for (int k = 0; k < 4; ++k) num[h2 * 4 + k] += f * v[k];
+            }
+        }
+        const float inv = 1.0f / den;
+        const u32x4 o = {pack_bf16x2(num[0] * inv, num[1] * inv), pack_bf16x2(num[2] * inv, num[3] * inv),
+                         pack_bf16x2(num[4] * inv, num[5] * inv), pack_bf16x2(num[6] * inv, num[7] * inv)};
+        if ((long)q_row0 + row < 0 || (long)q_row0 + row >= a.lse_rows) continue;
+        *reinterpret_cast<u32x4*>(a.out + ((size_t)(q_row0 + row) * a.n_q_heads + head) * HD + c * 8) = o;
+        if (a.lse && c == 0)
+            a.lse[(size_t)head * a.lse_rows + q_row0 + row] = mx * sl2 * 0.69314718055994531f + logf(den);
+    }
+}
+
+template <int HD, int W>
+hipError_t launch(const Attn8Args& b, bool compact, unsigned blocks, hipStream_t stream) {
+    if (compact)
+        hipLaunchKernelGGL((attn_split8_kernel<HD, W, true>), dim3(blocks), dim3(W * 64), 0, stream, b);
+    else
+        hipLaunchKernelGGL((attn_split8_kernel<HD, W, false>), dim3(blocks), dim3(W * 64), 0, stream, b);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attn_split8(const Attn8Args& a, int head_dim, int waves, hipStream_t stream) {
+    Attn8Args b = a;
+    const SplitGrid grid(b.a, waves);
+    if (grid.blocks <= 0) return hipSuccess;
+    if (grid.blocks > 0x7fffffffL) return hipErrorInvalidValue;
+    const unsigned n = (unsigned)grid.blocks;
+    if (head_dim == 128)
+        return waves == 8 ? launch<128, 8>(b, grid.compact, n, stream) : launch<128, 4>(b, grid.compact, n, stream);
+    return waves == 8 ? launch<64, 8>(b, grid.compact, n, stream) : launch<64, 4>(b, grid.compact, n, stream);
+}
+
+hipError_t launch_attn8(const Attn8Args& a, int head_dim, hipStream_t stream) {
+    if (a.a.ratio < 1 || a.a.max_rows < 1) return hipErrorInvalidValue;
+    const long col_blocks = std::max((a.a.lse_rows * a.a.ratio + 31) / 32, (long)a.a.n_units) * a.a.n_kv_heads;
+    return launch_attn_split8(a, head_dim, col_blocks <= 256 ? 8 : 4, stream);
+}
+
+}  // namespace rc

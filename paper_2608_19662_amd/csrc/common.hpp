@@ -136,4 +136,24 @@ __device__ __forceinline__ int segment_table(const int32_t* res, int n_seg, cons
     return __builtin_amdgcn_readfirstlane(carry);
 }
 
+// Work items of `unit` rows over segments of unknown lengths: segment s, whose
+// rows start at cu[s], has the items from cu[s] / unit + per * s on.  With per =
+// 1 those hold ceil(rows / unit) items of every segment, with 2 one more.  The
+// last s in [0, n) whose items start at `at` or before, by the 64 lanes of a
+// wave: each step tries 64 segments of the range at once.
+__device__ __forceinline__ long first_item(long row, int s, int unit, int per) { return row / unit + (long)per * s; }
+__device__ __forceinline__ int find_segment(const int32_t* cu, int n, int unit, int per, long at, int lane) {
+    int lo = 0, hi = n;  // the answer is in [lo, hi)
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) / 64;
+        const int s = lo + lane * step;
+        const bool le = s < hi && first_item(cu[s], s, unit, per) <= at;
+        // (lane 0 tries lo itself, which holds unless `at` is before every item)
+        const int k = max(__popcll(__builtin_amdgcn_ballot_w64(le)) - 1, 0);
+        lo = lo + k * step;
+        hi = min(hi, lo + step);
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
 }  // namespace rc

@@ -491,14 +491,21 @@ hipError_t launch_dec(const DecodeArgs& a, hipStream_t s) {
         hipLaunchKernelGGL((decode_kernel<HD, false, true>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
     else
         hipLaunchKernelGGL((decode_kernel<HD, false, false>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
-    hipError_t err = hipGetLastError();
-    if (err != hipSuccess) return err;
-    const unsigned waves = (unsigned)(a.n_req * a.n_q_heads), per = kThreads / 64;
-    hipLaunchKernelGGL((combine_kernel<HD>), dim3((waves + per - 1) / per), dim3(kThreads), 0, s, a);
-    return hipGetLastError();
+    const hipError_t err = hipGetLastError();
+    return err != hipSuccess ? err : launch_decode_merge(a, s);
 }
 
 }  // namespace
+
+hipError_t launch_decode_merge(const DecodeArgs& a, hipStream_t s) {
+    const unsigned waves = (unsigned)(a.n_req * a.n_q_heads), per = kThreads / 64;
+    const dim3 grid((waves + per - 1) / per), block(kThreads);
+    if (a.head_dim == 128)
+        hipLaunchKernelGGL((combine_kernel<128>), grid, block, 0, s, a);
+    else
+        hipLaunchKernelGGL((combine_kernel<64>), grid, block, 0, s, a);
+    return hipGetLastError();
+}
 
 namespace {
 

@@ -156,6 +156,103 @@ struct DecodeArgs {
     const int32_t* plan;  // work order of the (request, group) pairs, or NULL
 };
 hipError_t launch_decode(const DecodeArgs& a, hipStream_t stream);
+// The merge of the splits' partials in ws_o / ws_ml alone.
+hipError_t launch_decode_merge(const DecodeArgs& a, hipStream_t stream);
+
+// A cache in 8 bits beside the plane sizes of DecodeArgs / AttnArgs (whose own
+// K / V pointers are not used): codes, exponent bytes and scale slots.
+struct Cache8 {
+    const uint8_t* rk;  // resource rows
+    const uint8_t* rv;
+    const uint8_t* rk_exp;
+    const uint8_t* rv_exp;
+    long r_slots;    // scale slots of one KV head's part (all with res_off)
+    long r_sstride;  // slots between KV heads (0 with res_off)
+    const uint8_t* ck;  // context rows
+    const uint8_t* cv;
+    const uint8_t* ck_exp;
+    const uint8_t* cv_exp;
+    long c_slots;
+    const int32_t* ctx_len;  // context rows in use, or NULL (all)
+};
+struct Decode8Args : Cache8 {
+    DecodeArgs d;
+};
+hipError_t launch_decode8(const Decode8Args& a, hipStream_t stream);
+
+struct Attn8Args : Cache8 {
+    AttnArgs a;
+};
+// Prefill over caches in 8 bits.
+hipError_t launch_attn8(const Attn8Args& a, int head_dim, hipStream_t stream);
+hipError_t launch_attn_split8(const Attn8Args& a, int head_dim, int waves, hipStream_t stream);
+
+// Rows into the 8-bit cache format.
+struct QuantizeArgs {
+    int n_seg, n_planes;
+    const int32_t* cu;      // cache offsets of the segments
+    const int32_t* len;     // their rows in use, or NULL (all)
+    const int32_t* cu_new;  // offsets of their new rows in the source, or NULL (all rows, at cu)
+    long rows, n_slots;     // of a plane of the cache
+    long src_rows;
+    long n_blocks;  // bound on the blocks that new rows touch
+    const void* k;
+    const void* v;
+    long row_stride, plane_stride;  // of k and v, in elements
+    uint8_t* k8;
+    uint8_t* v8;
+    uint8_t* k_exp;
+    uint8_t* v_exp;
+};
+hipError_t launch_quantize(const QuantizeArgs& a, int elem_bytes, int head_dim, hipStream_t stream);
+
+// Attention weight that every cached row receives.
+struct WeighArgs {
+    int n_req, n_res, n_q_heads, n_kv_heads, ratio;
+    int one_query;  // every request has exactly one query
+    float scale_log2;
+    const void* q;
+    const float* lse;  // [n_q_heads][total_q]
+    long total_q;
+    const int32_t* cu_q;
+    const int32_t* cu_ctx;
+    const void* ck;
+    long c_rows;
+    const float* c_prior;  // or NULL (zeros)
+    float* c_w;            // or NULL (context not weighed)
+    const void* rk;
+    long r_rows;
+    const float* r_prior;
+    float* r_w;
+    const int32_t* cu_kept;
+    const int32_t* res_off;
+    const uint8_t* mask;  // [n_res][n_layers][n_kv_heads]
+    int layer, n_layers;
+    const int32_t* user_off;
+    const int32_t* user_req;
+    int n_users;
+    long r_items, c_items;  // the launcher's: bounds on key tiles, of a plane (of all with res_off)
+};
+hipError_t launch_weigh(const WeighArgs& a, int elem_bytes, int head_dim, hipStream_t stream);
+hipError_t launch_resource_users(int n_req, const int32_t* req_res_off, const int32_t* req_res, int total,
+                                 int n_res, int32_t* user_off, int32_t* user_req, hipStream_t stream);
+
+// The best-scored rows of every segment.
+struct SelectArgs {
+    int n_seg, n_planes;
+    const int32_t* cu;
+    long total;
+    const float* w;  // [n_planes][total]
+    const int32_t* cu_kept;
+    long total_kept;
+    int keep_first, keep_last, max_len;
+    int32_t* kept_idx;
+    float* kept_w;   // [n_planes][total_kept] or NULL
+    uint32_t* keys;  // long segments: scores in order-preserving form [total],
+                     // then the kept rows [total_kept]
+};
+hipError_t launch_select(const SelectArgs& a, hipStream_t stream);
+size_t select_workspace_bytes(long total, int max_len);
 int decode_splits(int n_req, int n_kv_heads, int max_kv);
 // The most partials per query head, requests times splits, that a batch of
 // n_req requests or any smaller one makes (a program that sizes its workspace

@@ -18,11 +18,13 @@ LIB_PATH = os.path.join(_HERE, "librecache.so")
 
 OK, EINVAL, EUNSUPPORTED, EWORKSPACE, EHIP = 0, -1, -2, -3, -4
 F32, BF16 = 0, 1
+BLOCK_TOKENS = 64  # tokens of an 8-bit cache that share a scale
 
 _lib = None
 
 _c_int, _c_dbl, _c_flt, _c_p, _c_size = (ctypes.c_int, ctypes.c_double, ctypes.c_float,
                                          ctypes.c_void_p, ctypes.c_size_t)
+_c_i64 = ctypes.c_int64
 
 _SIGS = {
     "recache_version": ([], _c_int),
@@ -56,6 +58,18 @@ _SIGS = {
                                        _c_int, _c_int, _c_int, _c_int, _c_int, _c_int, _c_flt, _c_p,
                                        _c_p, _c_p, _c_int, _c_p, _c_p, _c_int, _c_p, _c_p, _c_p,
                                        _c_p, _c_p, _c_p, _c_p, _c_p, _c_p], _c_int),
+    "recache_resource_users": ([_c_int, _c_p, _c_p, _c_int, _c_int, _c_p, _c_p, _c_p], _c_int),
+    "recache_attend_weights": ([_c_int] * 4 + [_c_p, _c_p] + [_c_int] * 5 + [_c_flt, _c_p, _c_p, _c_p, _c_int,
+                                _c_p, _c_p, _c_p, _c_int, _c_p, _c_p, _c_int, _c_p, _c_p, _c_p, _c_p,
+                                _c_p, _c_int, _c_p], _c_int),
+    "recache_select_workspace_bytes": ([_c_int] * 3, _c_size),
+    "recache_select_kept": ([_c_int, _c_p, _c_int, _c_int, _c_int, _c_p, _c_p, _c_int, _c_int, _c_int,
+                             _c_p, _c_p, _c_p, _c_size, _c_p], _c_int),
+    "recache_quantized_blocks": ([_c_int, _c_int], _c_size),
+    "recache_quantize_kv": ([_c_int, _c_int, _c_p, _c_p, _c_int, _c_int, _c_int, _c_p, _c_int, _c_p,
+                             _c_p, _c_i64, _c_i64, _c_p, _c_p, _c_p, _c_p, _c_p], _c_int),
+    "recache_attend_quantized": ([_c_int] * 4 + [_c_p] * 3 + [_c_int] * 8 + [_c_flt] + [_c_p] * 5 + [_c_int]
+                                 + [_c_p] * 4 + [_c_int, _c_int] + [_c_p] * 9 + [_c_size, _c_p], _c_int),
     "recache_select_routes": ([_c_int, _c_int, _c_p, _c_p, _c_int, _c_int, _c_p, _c_p, _c_p, _c_p,
                                _c_p, _c_p], _c_int),
     "recache_check_offsets": ([_c_p, _c_int, _c_int, _c_int], _c_int),
@@ -449,6 +463,209 @@ def attend_cached_noalloc(q, ctx_k, ctx_v, cu_q, cu_ctx, max_q: int, max_ctx: in
                         route_off, route_res, route_tokens, layer, n_layers, out, max_route_len,
                         lse, max_kv, softmax_scale, res_off, plan)
     _call("recache_attend_cached_noalloc", *args, _stream(stream))
+
+
+# ------------------------------------------------ eviction by attention weight
+
+def _f32():
+    return (torch or _torch()).float32,
+
+
+def resource_users(req_res_off, req_res, n_res: int, user_off, user_req, stream=None):
+    """Inverse of the request lists: the requests that list each resource
+    (user_off[n_res + 1], user_req[total], int32)."""
+    n = req_res.numel()
+    _numel(user_off, "user_off", n_res + 1)
+    _numel(req_res, "req_res", n)
+    _at_least(user_req, "user_req", n)
+    _call("recache_resource_users", req_res_off.numel() - 1, _dev(req_res_off, "req_res_off", _i32()),
+          _dev(req_res, "req_res", _i32()), n, int(n_res), _dev(user_off, "user_off", _i32()),
+          _dev(user_req, "user_req", _i32()), _stream(stream))
+
+
+def attend_weights(q, lse, cu_q, cu_ctx, max_q: int, cu_kept, route_mask, user_off, user_req, layer: int,
+                   *, ctx_k=None, ctx_w=None, ctx_w_prior=None, res_k=None, res_w=None, res_w_prior=None,
+                   res_off=None, softmax_scale: float = 0.0, stream=None):
+    """Attention weight that every cached row receives in one layer (see recache.h).
+
+    ctx_k [Hkv][rows][d] with ctx_w [Hkv][rows], res_k [Hkv][rows][d] with res_w
+    [Hkv][rows] (or a store [rows][d] with [rows]); either pair may be left
+    out.  The priors are added (None: zeros; the outputs themselves: in place).
+    cu_kept, route_mask, user_off and user_req are for resources only."""
+    total_q, Hq, d = q.shape
+    n_req = cu_q.numel() - 1
+    _numel(cu_ctx, "cu_ctx", n_req + 1)
+    _shape(lse, "lse", Hq, total_q)
+    n_res, n_layers, n_users, ctx_rows, res_rows = 0, max(int(layer) + 1, 1), 0, 0, 0
+    if (ctx_w is None) != (ctx_k is None) or (res_w is None) != (res_k is None):
+        raise ValueError("ctx_k with ctx_w and res_k with res_w: both or neither")
+    if ctx_w is None and res_w is None:
+        raise ValueError("neither ctx_w nor res_w")
+    if route_mask is not None:
+        Hkv = route_mask.shape[2]
+    else:
+        Hkv = ctx_k.shape[0] if ctx_k is not None else 0
+    if ctx_w is not None:
+        _same(q, ctx_k)
+        if ctx_k.dim() != 3 or ctx_k.shape[0] != Hkv or ctx_k.shape[2] != d:
+            raise ValueError("ctx_k must be [%d][rows][%d], has shape %s" % (Hkv, d, tuple(ctx_k.shape)))
+        ctx_rows = ctx_k.shape[1]
+        _shape(ctx_w, "ctx_w", Hkv, ctx_rows)
+        _shape(ctx_w_prior, "ctx_w_prior", Hkv, ctx_rows)
+    if res_w is not None:
+        if cu_kept is None or route_mask is None or user_off is None or user_req is None:
+            raise ValueError("res_w needs cu_kept, route_mask, user_off and user_req")
+        _same(q, res_k)
+        n_res, n_layers, n_users = route_mask.shape[0], route_mask.shape[1], user_req.numel()
+        _numel(cu_kept, "cu_kept", n_res + 1)
+        _numel(user_off, "user_off", n_res + 1)
+        if res_off is not None:
+            _numel(res_off, "res_off", n_res * Hkv + 1)
+            if res_k.dim() != 2 or res_k.shape[1] != d:
+                raise ValueError("a route-compacted store is [rows][%d], res_k has shape %s"
+                                 % (d, tuple(res_k.shape)))
+            res_rows = res_k.shape[0]
+        else:
+            if res_k.dim() != 3 or res_k.shape[0] != Hkv or res_k.shape[2] != d:
+                raise ValueError("res_k must be [%d][rows][%d], has shape %s" % (Hkv, d, tuple(res_k.shape)))
+            res_rows = res_k.shape[1]
+        _shape(res_w, "res_w", *res_k.shape[:-1])
+        _shape(res_w_prior, "res_w_prior", *res_k.shape[:-1])
+    f32 = _f32()
+    _call("recache_attend_weights", _dtype_code(q), int(layer), n_layers, n_req, _dev(cu_q, "cu_q", _i32()),
+          _dev(cu_ctx, "cu_ctx", _i32()), total_q, int(max_q), Hq, Hkv, d, softmax_scale, _dev(q, "q"),
+          _dev(lse, "lse", f32), _dev(ctx_k, "ctx_k"), ctx_rows, _dev(ctx_w_prior, "ctx_w_prior", f32),
+          _dev(ctx_w, "ctx_w", f32), _dev(res_k, "res_k"), res_rows, _dev(res_w_prior, "res_w_prior", f32),
+          _dev(res_w, "res_w", f32), n_res, _dev(cu_kept, "cu_kept", _i32()), _dev(res_off, "res_off", _i32()),
+          _dev(route_mask, "route_mask", _u8()), _dev(user_off, "user_off", _i32()),
+          _dev(user_req, "user_req", _i32()), n_users, _stream(stream))
+
+
+def select_workspace_bytes(n_seg: int, total: int, max_len: int) -> int:
+    return int(lib().recache_select_workspace_bytes(n_seg, total, max_len))
+
+
+def select_kept(w, cu, cu_kept, kept_idx, *, max_len: int, kept_w=None, keep_first: int = 0, keep_last: int = 1,
+                workspace=None, stream=None):
+    """Kept lists by score: the best rows of every segment by the sum of
+    w[planes][total] over the planes (see recache.h); kept_idx [total_kept],
+    kept_w [planes][total_kept] or None."""
+    planes, total = w.shape
+    n_seg = cu.numel() - 1
+    K = kept_idx.numel()
+    _numel(cu_kept, "cu_kept", n_seg + 1)
+    _numel(kept_idx, "kept_idx", K)
+    _shape(kept_w, "kept_w", planes, K)
+    f32 = _f32()
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _call("recache_select_kept", n_seg, _dev(cu, "cu", _i32()), total, int(max_len), planes, _dev(w, "w", f32),
+          _dev(cu_kept, "cu_kept", _i32()), K, int(keep_first), int(keep_last), _dev(kept_idx, "kept_idx", _i32()),
+          _dev(kept_w, "kept_w", f32), _dev(workspace, "workspace"), ws_bytes, _stream(stream))
+
+
+# ------------------------------------------------------------- 8-bit caches
+
+def _codes(t, name, *dims):
+    """Device pointer of e4m3 codes (float8_e4m3fn, or their bytes as uint8)."""
+    _shape(t, name, *dims)
+    return _dev(t, name, ((torch or _torch()).float8_e4m3fn, torch.uint8))
+
+
+def quantized_blocks(rows: int, n_seg: int) -> int:
+    """Scale bytes of a plane of an 8-bit cache of n_seg segments."""
+    return int(lib().recache_quantized_blocks(rows, n_seg))
+
+
+def quantize_kv(k, v, k8, v8, k_exp, v_exp, cu, *, lens=None, cu_new=None, stream=None):
+    """K/V rows into an 8-bit cache (see recache.h).
+
+    k, v: [planes][rows][d] of any plane and row strides (a cache, a store as
+    one plane, a projection [rows][heads][d] as k.transpose(0, 1)); k8, v8:
+    codes [planes][cache rows][d]; k_exp, v_exp: uint8 [planes][blocks].  The
+    rows are those of the segments cu, or with cu_new their newest ones; lens:
+    rows of each segment in use, where it has room for more."""
+    if k.dim() != 3 or v.shape != k.shape:
+        raise ValueError("k and v must be [planes][rows][d] of one shape, have %s, %s"
+                         % (tuple(k.shape), tuple(v.shape)))
+    planes, src_rows, d = k.shape
+    # (a dimension of one has no stride that counts)
+    row_stride = k.stride(1) if src_rows > 1 else 0
+    plane_stride = k.stride(0) if planes > 1 else 0
+    if (src_rows > 1 and v.stride(1) != row_stride) or (planes > 1 and v.stride(0) != plane_stride):
+        raise ValueError("k and v must have one layout, have strides %s, %s" % (k.stride(), v.stride()))
+    n_seg = cu.numel() - 1
+    if k8.dim() != 3 or k8.shape[0] != planes or k8.shape[2] != d:
+        raise ValueError("k8 must be [%d][rows][%d], has shape %s" % (planes, d, tuple(k8.shape)))
+    rows = k8.shape[1]
+    if cu_new is None and src_rows != rows:
+        raise ValueError("without cu_new the source has the cache's %d rows, not %d" % (rows, src_rows))
+    _same(k, v)
+    _numel(lens, "lens", n_seg)
+    _numel(cu_new, "cu_new", n_seg + 1)
+    blocks = rows // BLOCK_TOKENS + n_seg
+    _shape(k_exp, "k_exp", planes, blocks)
+    _shape(v_exp, "v_exp", planes, blocks)
+    for t, name in ((k, "k"), (v, "v")):
+        if not t.is_cuda:
+            raise TypeError("%s must be a CUDA tensor" % name)
+        if t.numel() and t.stride(2) != 1:
+            raise ValueError("the elements of a row of %s must be contiguous" % name)
+    _call("recache_quantize_kv", _dtype_code(k), n_seg, _dev(cu, "cu", _i32()), _dev(lens, "lens", _i32()), rows,
+          planes, d, _dev(cu_new, "cu_new", _i32()), src_rows, k.data_ptr(), v.data_ptr(), row_stride, plane_stride,
+          _codes(k8, "k8", planes, rows, d), _codes(v8, "v8", planes, rows, d), _dev(k_exp, "k_exp", _u8()),
+          _dev(v_exp, "v_exp", _u8()), _stream(stream))
+
+
+def attend_quantized(q, ctx_k, ctx_v, ctx_k_exp, ctx_v_exp, cu_q, cu_ctx, max_q: int, max_ctx: int, res_k, res_v,
+                     res_k_exp, res_v_exp, cu_kept, route_off, route_res, route_tokens, layer: int, n_layers: int,
+                     out, *, max_route_len: int, ctx_len=None, lse=None, workspace=None, max_kv: int = 0,
+                     softmax_scale: float = 0.0, res_off=None, plan=None, stream=None):
+    """attend_cached over 8-bit caches: codes as in quantize_kv, context
+    [Hkv][rows][d] with exponents [Hkv][blocks], resources likewise, or a store
+    [rows][d] with [blocks] (res_off).  ctx_len: context rows in use."""
+    total_q, Hq, d = q.shape
+    if ctx_k.dim() != 3 or ctx_k.shape[2] != d:
+        raise ValueError("ctx_k must be [Hkv][rows][%d], has shape %s" % (d, tuple(ctx_k.shape)))
+    Hkv, ctx_rows = ctx_k.shape[0], ctx_k.shape[1]
+    n_req = cu_q.numel() - 1
+    n_res = cu_kept.numel() - 1
+    E = n_req * n_layers * Hkv
+    _same(q, out)
+    _shape(out, "out", total_q, Hq, d)
+    _shape(lse, "lse", Hq, total_q)
+    _numel(cu_ctx, "cu_ctx", n_req + 1)
+    _numel(ctx_len, "ctx_len", n_req)
+    _numel(route_off, "route_off", E + 1)
+    _numel(route_tokens, "route_tokens", E)
+    _shape(plan, "plan", n_layers, n_req * Hkv)
+    blocks = ctx_rows // BLOCK_TOKENS + n_req
+    _shape(ctx_k_exp, "ctx_k_exp", Hkv, blocks)
+    _shape(ctx_v_exp, "ctx_v_exp", Hkv, blocks)
+    if res_off is not None:
+        _numel(res_off, "res_off", n_res * Hkv + 1)
+        if res_k.dim() != 2 or res_k.shape[1] != d:
+            raise ValueError("a route-compacted store is [rows][%d], res_k has shape %s" % (d, tuple(res_k.shape)))
+        res_rows = res_k.shape[0]
+        exp_shape = (res_rows // BLOCK_TOKENS + n_res * Hkv,)
+    else:
+        if res_k.dim() != 3 or res_k.shape[0] != Hkv or res_k.shape[2] != d:
+            raise ValueError("res_k must be [%d][rows][%d], has shape %s" % (Hkv, d, tuple(res_k.shape)))
+        res_rows = res_k.shape[1]
+        exp_shape = (Hkv, res_rows // BLOCK_TOKENS + n_res)
+    _shape(res_k_exp, "res_k_exp", *exp_shape)
+    _shape(res_v_exp, "res_v_exp", *exp_shape)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _call("recache_attend_quantized", _dtype_code(q), layer, n_layers, n_req, _dev(cu_q, "cu_q", _i32()),
+          _dev(cu_ctx, "cu_ctx", _i32()), _dev(ctx_len, "ctx_len", _i32()), total_q, int(max_q), int(max_ctx),
+          int(max_kv), int(max_route_len), Hq, Hkv, d, softmax_scale, _dev(q, "q"),
+          _codes(ctx_k, "ctx_k", Hkv, ctx_rows, d), _codes(ctx_v, "ctx_v", Hkv, ctx_rows, d),
+          _dev(ctx_k_exp, "ctx_k_exp", _u8()), _dev(ctx_v_exp, "ctx_v_exp", _u8()), ctx_rows,
+          _codes(res_k, "res_k", *res_k.shape), _codes(res_v, "res_v", *res_k.shape),
+          _dev(res_k_exp, "res_k_exp", _u8()), _dev(res_v_exp, "res_v_exp", _u8()), res_rows, n_res,
+          _dev(cu_kept, "cu_kept", _i32()), _dev(res_off, "res_off", _i32()), _dev(route_off, "route_off", _i32()),
+          _dev(route_res, "route_res", _i32()), _dev(route_tokens, "route_tokens", _i32()),
+          _dev(plan, "plan", _i32()), _dev(out, "out"), _dev(lse, "lse", _f32()), _dev(workspace, "workspace"),
+          ws_bytes, _stream(stream))
 
 
 def check_offsets(cu, total: int, strict: bool = True) -> None:

@@ -1,0 +1,373 @@
+"""Eviction by accumulated attention weight on the GPU: attend_weights against
+64 bits, the inverse request lists and the kept lists exactly.
+
+Tolerance of a weight, a sum of n positive terms exp(s - lse) in fp32, relative:
+a logit is a sum of d products whose absolute values (times the scale) sum to at
+most A, off by d 2^-24 A; s and lse in units of log2(e), their difference and the
+stored lse are off by 2^-23 (|s| + 2 |lse|) together; the exponential by 2^-22;
+the sum by n 2^-24.  With d <= 128, A <= 20, |s| <= 20, |lse| <= 20 and n <= 10000 that
+is under 153e-6 + 8e-6 + 596e-6 < 8e-4; errors of a sum add up from both signs, and what is
+seen is far less, so the bound is taken with the actual n."""
+import numpy as np
+import pytest
+import torch
+
+import cache_reference as ref
+from gpu_helpers import DEV, Routes, check, f64, i32
+from paper_2608_19662_amd import recache as rc
+from paper_2608_19662_amd.workloads import AttendWorkload, EncodeWorkload, prefix
+from test_gpu_parity import small_attend
+
+pytestmark = pytest.mark.gpu
+
+
+def bound(w, prior):
+    n = int(np.sum(w.q_lens)) * (w.n_q_heads // w.n_kv_heads)
+    return (153 + 8) * 1e-6 + (n + 2 * prior) * 2.0 ** -24
+
+
+def gpu_users(w):
+    uo = torch.empty(w.n_res + 1, dtype=torch.int32, device=DEV)
+    ur = torch.empty(max(len(w.req_res), 1), dtype=torch.int32, device=DEV)
+    rc.resource_users(i32(w.req_res_off), i32(w.req_res), w.n_res, uo, ur)
+    return uo, ur[:len(w.req_res)] if len(w.req_res) else ur
+
+
+class Weigh:
+    def __init__(self, w, layer, store=False):
+        self.w, self.layer = w, layer
+        self.q, self.ck, self.cv, rk, rv = w.layer_tensors(layer, DEV)
+        self.rt = Routes(w)
+        self.res_off = self.seg_off = None
+        if store:
+            off = self.rt.store_offsets()
+            self.res_off, self.seg_off = off[layer], off[layer].cpu().numpy()
+            rows = int(self.seg_off[-1])
+            ks, vs = (torch.zeros(rows, w.head_dim, dtype=rk.dtype, device=DEV) for _ in "kv")
+            if rows:
+                rc.store_routes(rk, rv, self.rt.cu_rows, self.rt.cu_rows,
+                                i32(np.concatenate([np.arange(n) for n in np.diff(w.cu_rows)])), off, layer, ks, vs,
+                                total_kept=int(w.cu_rows[-1]))
+            rk, rv = ks, vs
+        self.rk, self.rv = rk, rv
+        q64 = self.q.cpu().double().numpy()
+        h = lambda t: t.cpu().double().numpy()
+        _, lse, _ = ref.attend(w, q64, h(rk), h(rv), h(self.ck), h(self.cv), layer, seg_off=self.seg_off)
+        self.lse = torch.from_numpy(lse).float().to(DEV)
+        self.want = ref.attend_weights(w, q64, self.lse.cpu().double().numpy(), h(rk), h(self.ck), layer,
+                                       seg_off=self.seg_off)
+
+    def run(self, prior=None, res=True, ctx=True, in_place=False, stream=None):
+        w = self.w
+        rw = torch.full(self.rk.shape[:-1], float("nan"), device=DEV)
+        cw = torch.full(self.ck.shape[:-1], float("nan"), device=DEV)
+        rp = cp = None
+        if prior is not None:
+            rp, cp = torch.full_like(rw, prior), torch.full_like(cw, prior)
+            if in_place:
+                rw, cw = rp, cp
+        rc.attend_weights(self.q, self.lse, self.rt.cu_q, self.rt.cu_ctx, self.rt.max_q, self.rt.cu_rows, self.rt.mask,
+                          *gpu_users(w), self.layer, ctx_k=self.ck if ctx else None, ctx_w=cw if ctx else None,
+                          ctx_w_prior=cp if ctx else None, res_k=self.rk if res else None, res_w=rw if res else None,
+                          res_w_prior=rp if res else None, res_off=self.res_off if res else None, stream=stream)
+        torch.cuda.synchronize()
+        return rw, cw
+
+    def check(self, rw, cw, prior=0.0):
+        for got, want, name in ((rw, self.want[0], "res"), (cw, self.want[1], "ctx")):
+            want = want + prior
+            err = np.abs(f64(got) - want)
+            tol = bound(self.w, prior != 0) * want + 1e-30
+            assert (err <= tol).all(), (name, float((err / tol).max()), np.argwhere(~(err <= tol))[:3])
+
+
+HEADS = [(32, 8, 128, "bf16"), (8, 2, 64, "bf16"), (28, 4, 128, "bf16"), (8, 8, 128, "bf16"), (12, 4, 64, "bf16"),
+         (32, 8, 128, "f32"), (12, 4, 64, "f32"), (40, 2, 64, "f32")]
+
+
+@pytest.mark.parametrize("store", [False, True])
+@pytest.mark.parametrize("q,ctx", [([1] * 6, [1, 63, 64, 65, 700, 129]), ([1, 33, 64, 2, 70, 9], [1, 33, 130, 65, 200, 9])])
+@pytest.mark.parametrize("Hq,Hkv,d,dtype", HEADS)
+def test_weights(Hq, Hkv, d, dtype, q, ctx, store):
+    w = small_attend(13 + Hq, 6, 9, Hq, Hkv, d, dtype, q, ctx, max_len=400)
+    x = Weigh(w, 1, store)
+    rw, cw = x.run()
+    x.check(rw, cw)
+    again = x.run()
+    assert torch.equal(rw, again[0]) and torch.equal(cw, again[1])
+    # accumulation, beside the prior and in place
+    for in_place in (False, True):
+        rw2, cw2 = x.run(prior=2.5, in_place=in_place)
+        x.check(rw2, cw2, prior=2.5)
+    # either half alone
+    assert torch.equal(x.run(ctx=False)[0], rw) and torch.equal(x.run(res=False)[1], cw)
+
+
+def test_weights_of_many_users():
+    """One resource read by 200 requests of one query and by 60 of several, listed twice by one."""
+    for q, n in ((1, 200), (3, 60)):
+        rng = np.random.default_rng(n)
+        lists = [[0] if b % 3 else [1, 0] for b in range(n)]
+        lists[5] = [0, 1, 0]
+        lists[6] = []
+        w = AttendWorkload(seed=n, n_layers=2, n_q_heads=8, n_kv_heads=2, head_dim=128, dtype="bf16",
+                           lengths=np.array([70, 130, 5], np.int32), req_res_off=prefix([len(x) for x in lists]),
+                           req_res=np.concatenate(lists).astype(np.int32), q_lens=np.full(n, q, np.int32),
+                           ctx_lens=rng.integers(q, 80, n).astype(np.int32), mask=np.ones((3, 2, 2), np.uint8))
+        x = Weigh(w, 1)
+        x.check(*x.run())
+
+
+def test_weights_of_nobody():
+    """Requests without resources; resources without users and routes get their prior."""
+    w = AttendWorkload(seed=3, n_layers=1, n_q_heads=8, n_kv_heads=2, head_dim=128, dtype="bf16",
+                       lengths=np.array([65, 3], np.int32), req_res_off=np.array([0, 0, 0], np.int32),
+                       req_res=np.zeros(0, np.int32), q_lens=np.array([4, 90], np.int32),
+                       ctx_lens=np.array([4, 90], np.int32), mask=np.array([[[1, 0]], [[0, 1]]], np.uint8))
+    x = Weigh(w, 0)
+    rw, cw = x.run()
+    assert (rw == 0).all()
+    x.check(rw, cw)
+    rw, cw = x.run(prior=0.75)
+    assert (rw == 0.75).all()
+
+
+def test_weights_leave_other_rows_alone():
+    """Rows behind the last resource and context keep what they held."""
+    w = small_attend(71, 3, 4, 8, 2, 64, "bf16", [5, 1, 40], [10, 1, 70])
+    x = Weigh(w, 0)
+    extra = lambda t: torch.cat([t, torch.full((2, 77, 64), float("nan"), dtype=t.dtype, device=DEV)], 1).contiguous()
+    x.rk, x.ck = extra(x.rk), extra(x.ck)
+    rw, cw = x.run(prior=1.0, in_place=True)
+    assert (rw[:, -77:] == 1.0).all() and (cw[:, -77:] == 1.0).all()
+    x.check(rw[:, :-77], cw[:, :-77], prior=1.0)
+
+
+def test_weights_nan_and_infinity_stay_where_they_are_seen():
+    w = small_attend(73, 2, 3, 8, 2, 64, "bf16", [30, 20], [60, 20], mask_p=1.0)
+    w.req_res_off, w.req_res = prefix([1, 1]), np.array([0, 1], np.int32)
+    x = Weigh(w, 0)
+    x.ck[0, 59, 3] = float("nan")   # the newest key of request 0: seen by its last query only
+    x.ck[1, 79, 3] = float("inf")   # the newest key of request 1
+    x.rk[1, int(w.cu_rows[2]):] = float("nan")  # a resource that nobody lists
+    rw, cw = x.run()
+    assert torch.isnan(cw[0, 59]) and not torch.isfinite(cw[1, 79])
+    cw[0, 59] = cw[1, 79] = 0
+    x.want[1][0, 59] = x.want[1][1, 79] = 0
+    x.check(rw, cw)
+
+
+def test_weights_of_a_decode_call_with_two_queries_are_nan():
+    w = small_attend(75, 2, 2, 4, 2, 64, "bf16", [1, 1], [30, 40], mask_p=1.0)
+    w.req_res_off, w.req_res = prefix([1, 1]), np.array([0, 1], np.int32)
+    x = Weigh(w, 0)
+    x.rt.cu_q = i32([0, 2, 2])
+    rw, _ = x.run(ctx=False)
+    assert torch.isnan(rw[:, :int(w.cu_rows[1])]).all()
+
+
+def test_weights_from_the_librarys_own_lse():
+    """The attention call's LSE is that of bf16-rounded weights: every query
+    gives away 1, within 2^-8 and the fp32 terms."""
+    w = small_attend(79, 4, 6, 32, 8, 128, "bf16", [1, 40, 64, 7], [90, 40, 200, 8])
+    x = Weigh(w, 2)
+    _, lse = x.rt.attend(x.q, x.ck, x.cv, x.rk, x.rv, 2, max_kv=x.rt.max_kv(2))
+    x.lse = lse
+    rw, cw = x.run()
+    total = float(rw.double().sum() + cw.double().sum())
+    assert abs(total / (112 * 32) - 1) <= 2.0 ** -8 + 8e-4
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_resource_users(seed):
+    rng = np.random.default_rng(seed)
+    n_req, n_res = int(rng.integers(1, 90)), int(rng.integers(1, 300))
+    lists = [rng.integers(0, n_res, rng.integers(0, 40)) for _ in range(n_req)]  # (the same one twice, too)
+    w = AttendWorkload(seed=1, n_layers=1, n_q_heads=1, n_kv_heads=1, head_dim=64, dtype="bf16",
+                       lengths=np.ones(n_res, np.int32), req_res_off=prefix([len(x) for x in lists]),
+                       req_res=np.concatenate(lists).astype(np.int32), q_lens=np.ones(n_req, np.int32),
+                       ctx_lens=np.ones(n_req, np.int32), mask=np.ones((n_res, 1, 1), np.uint8))
+    off, req = gpu_users(w)
+    torch.cuda.synchronize()
+    wo, wr = ref.users(w.req_res_off, w.req_res, n_res)
+    assert np.array_equal(off.cpu().numpy(), wo)
+    if len(wr):
+        assert np.array_equal(req.cpu().numpy(), wr)
+
+
+# ------------------------------------------------------------------- select_kept
+
+def scores(rng, planes, total, kind):
+    w = np.exp(rng.normal(size=(planes, total)))
+    if kind == "ties":
+        w = rng.integers(0, 4, (planes, total)).astype(np.float64)
+    elif kind == "equal":
+        w[:] = 0.5
+    elif kind == "signs":
+        w = rng.normal(size=(planes, total))
+        w[:, ::11] = 0.0
+        w[:, 1::11] = -0.0
+    elif kind == "odd":
+        w[:, rng.random(total) < 0.1] = np.nan
+        w[0, rng.random(total) < 0.05] = np.inf
+        w[0, rng.random(total) < 0.05] = -np.inf
+        w[:, rng.random(total) < 0.05] = 1e-44  # subnormal
+    return w.astype(np.float32)
+
+
+def run_select(w, cu, cu_kept, first, last, max_len=None, weights=True, stream=None):
+    K = int(cu_kept[-1])
+    n = max_len or int(np.diff(cu).max())
+    idx = torch.full((K,), -7, dtype=torch.int32, device=DEV)
+    kw = torch.full((w.shape[0], K), -7.0, device=DEV) if weights else None
+    ws = torch.empty(rc.select_workspace_bytes(len(cu) - 1, w.shape[1], n) or 1, dtype=torch.uint8, device=DEV)
+    rc.select_kept(torch.from_numpy(w).to(DEV), i32(cu), i32(cu_kept), idx, max_len=n, kept_w=kw, keep_first=first,
+                   keep_last=last, workspace=ws, stream=stream)
+    torch.cuda.synchronize()
+    return idx.cpu().numpy(), kw.cpu().numpy() if weights else None
+
+
+@pytest.mark.parametrize("max_len", [None, 5000, 20000])
+@pytest.mark.parametrize("kind", ["plain", "ties", "equal", "signs", "odd"])
+@pytest.mark.parametrize("planes,first,last", [(8, 0, 1), (1, 4, 0), (3, 2, 70)])
+def test_select(planes, first, last, kind, max_len):
+    """Segments of none to some thousands of rows; keeping none, all and in
+    between; by every form of the kernel (max_len chooses it)."""
+    rng = np.random.default_rng(planes)
+    lens = np.array([1, 2, 63, 64, 65, 0, 255, 256, 257, 1000, 3, 4095, 4096, 40] + list(rng.integers(0, 300, 20)))
+    if max_len == 20000:  # (max_len is at most the rows there are)
+        lens = np.append(lens, [9000, 11])
+    k = np.array([rng.integers(0, n + 1) for n in lens])
+    k[:5] = lens[:5]
+    k[7] = 0
+    cu, cu_kept = prefix(lens), prefix(k)
+    w = scores(rng, planes, int(cu[-1]), kind)
+    idx, kw = run_select(w, cu, cu_kept, first, last, max_len)
+    want, want_w = ref.select(w, cu, cu_kept, first, last)
+    assert np.array_equal(idx, want)
+    assert np.array_equal(kw, want_w, equal_nan=True)
+
+
+@pytest.mark.parametrize("lens", [[5000, 3, 4097], [16384, 100], [16385, 1, 0, 70000], [200001]])
+def test_select_long(lens):
+    rng = np.random.default_rng(len(lens))
+    lens = np.array(lens)
+    k = np.maximum(lens // 4, np.minimum(lens, 1))
+    cu, cu_kept = prefix(lens), prefix(k)
+    for kind in ("plain", "ties"):
+        w = scores(rng, 4, int(cu[-1]), kind)
+        idx, kw = run_select(w, cu, cu_kept, 4, 64)
+        want, want_w = ref.select(w, cu, cu_kept, 4, 64)
+        assert np.array_equal(idx, want)
+        assert np.array_equal(kw, want_w)
+        assert np.array_equal(run_select(w, cu, cu_kept, 4, 64, weights=False)[0], want)
+
+
+def test_select_longer_than_max_len():
+    """A segment that is longer than max_len says is marked, the others are right."""
+    rng = np.random.default_rng(8)
+    for lens, max_len in (([30, 5000, 40], 60), ([30, 17000, 40], 5000), ([30, 40000, 40], 17000)):
+        cu, cu_kept = prefix(lens), prefix([10, 20, 30])
+        w = scores(rng, 2, int(cu[-1]), "plain")
+        idx, kw = run_select(w, cu, cu_kept, 0, 1, max_len)
+        want, want_w = ref.select(w, cu, cu_kept, 0, 1)
+        assert (idx[10:30] == -1).all() and np.isnan(kw[:, 10:30]).all()
+        for a, z in ((0, 10), (30, 60)):
+            assert np.array_equal(idx[a:z], want[a:z]) and np.array_equal(kw[:, a:z], want_w[:, a:z])
+
+
+# ------------------------------------------------------------- the run of them
+
+def test_shrinking_a_cache_as_it_is_used():
+    """Encode resources, let a prompt attend to them, weigh their rows, keep the
+    best, put what stays into 8 bits, and decode over it."""
+    lengths = np.array([40, 129, 300, 64, 7], np.int32)
+    Hq, Hkv, d, L = 8, 2, 128, 2
+    rng = np.random.default_rng(2)
+    enc = EncodeWorkload(seed=5, lengths=lengths, n_q_heads=Hq, n_kv_heads=Hkv, head_dim=d, dtype="bf16", rope_base=1e6)
+    q, k, v = enc.tensors(DEV)
+    kc, vc = (torch.empty(Hkv, enc.total, d, dtype=torch.bfloat16, device=DEV) for _ in "kv")
+    cu_len = i32(enc.cu_len)
+    rc.encode_resources(q, k, v, cu_len, 300, 1e6, torch.empty_like(q), kc, vc)
+    w = AttendWorkload(seed=6, n_layers=L, n_q_heads=Hq, n_kv_heads=Hkv, head_dim=d, dtype="bf16", lengths=lengths,
+                       req_res_off=np.array([0, 3, 5], np.int32), req_res=np.array([2, 0, 4, 1, 2], np.int32),
+                       q_lens=np.array([40, 70], np.int32), ctx_lens=np.array([90, 70], np.int32),
+                       mask=(rng.random((5, L, Hkv)) < 0.8).astype(np.uint8))
+    rt = Routes(w)
+    uo, ur = gpu_users(w)
+    total = torch.zeros(Hkv, enc.total, device=DEV)
+    ctx_w = torch.zeros(Hkv, 160, device=DEV)
+    for layer in range(L):  # (the layers share a cache here; a program has one of each)
+        cq, ck, cv, _, _ = w.layer_tensors(layer, DEV)
+        out, lse = rt.attend(cq, ck, cv, kc, vc, layer, max_kv=rt.max_kv(layer))
+        rc.attend_weights(cq, lse, rt.cu_q, rt.cu_ctx, rt.max_q, rt.cu_rows, rt.mask, uo, ur, layer, ctx_k=ck,
+                          ctx_w=ctx_w, ctx_w_prior=ctx_w, res_k=kc, res_w=total, res_w_prior=total)
+    assert abs(float(total.double().sum() + ctx_w.double().sum()) / (110 * Hq * L) - 1) <= 2.0 ** -8 + 8e-4
+    # kept lists of resources and contexts
+    kept_n = np.maximum(1, lengths * 3 // 10)
+    cu_kept = prefix(kept_n)
+    kept = torch.empty(int(cu_kept[-1]), dtype=torch.int32, device=DEV)
+    rc.select_kept(total, cu_len, i32(cu_kept), kept, max_len=300)
+    torch.cuda.synchronize()
+    want, _ = ref.select(total.cpu().numpy(), enc.cu_len, cu_kept, 0, 1)
+    assert np.array_equal(kept.cpu().numpy(), want)
+    rc.check_kept(enc.cu_len, cu_kept, want)
+    cu_c = prefix([30, 70])
+    kept_c = torch.empty(100, dtype=torch.int32, device=DEV)
+    rc.select_kept(ctx_w, rt.cu_ctx, i32(cu_c), kept_c, max_len=90, keep_first=4, keep_last=8)
+    # compaction, 8 bits
+    caches = []
+    for c, cu0, cu1, idx in (((kc, vc), enc.cu_len, cu_kept, kept), ((ck, cv), w.cu_ctx, cu_c, kept_c)):
+        kk, vk = (torch.empty(Hkv, int(cu1[-1]), d, dtype=torch.bfloat16, device=DEV) for _ in "kv")
+        rc.prune_gather(*c, i32(cu0), i32(cu1), idx, kk, vk)
+        c8 = [torch.empty(kk.shape, dtype=torch.uint8, device=DEV) for _ in "kv"]
+        e8 = [torch.zeros(Hkv, rc.quantized_blocks(kk.shape[1], len(cu1) - 1), dtype=torch.uint8, device=DEV) for _ in "kv"]
+        rc.quantize_kv(kk, vk, *c8, *e8, i32(cu1))
+        caches.append((*c8, *e8, *(ref.dequantize(c.cpu().numpy(), e.cpu().numpy(), cu1) for c, e in zip(c8, e8))))
+    # one new token of both requests over what is left
+    w2 = AttendWorkload(**{**w.__dict__, "q_lens": np.ones(2, np.int32), "ctx_lens": np.array([30, 70], np.int32),
+                           "cu_kept": cu_kept, "kept_idx": want})
+    rt2 = Routes(w2)
+    cq = w2.layer_tensors(1, DEV)[0]
+    out = torch.empty_like(cq)
+    (rk, rv, rke, rve, rk64, rv64), (ck, cv, cke, cve, ck64, cv64) = caches
+    rc.attend_quantized(cq, ck, cv, cke, cve, rt2.cu_q, rt2.cu_ctx, 1, 70, rk, rv, rke, rve, rt2.cu_rows, rt2.route_off,
+                        rt2.route_res, rt2.route_tokens, 1, L, out, max_route_len=3, workspace=rt2.workspace(rt2.max_kv(1)),
+                        max_kv=rt2.max_kv(1))
+    torch.cuda.synchronize()
+    o, _, spread = ref.attend(w2, cq.cpu().double().numpy(), rk64, rv64, ck64, cv64, 1)
+    err = np.abs(f64(out) - o)
+    assert (err <= (2.0 ** -8 * 1.005 + 7e-4) * spread + (2.0 ** -8 + 7e-4) * np.abs(o) + 1e-6).all()
+
+
+def test_weights_and_selection_in_a_graph():
+    """Accumulate and select, captured and replayed on another stream's inputs;
+    every replay against the eager calls."""
+    w = small_attend(83, 3, 5, 8, 2, 64, "bf16", [1, 1, 1], [60, 1, 300], max_len=300)
+    x = Weigh(w, 0)
+    uo, ur = gpu_users(w)
+    lens = np.diff(w.cu_rows)
+    cu_kept = prefix(np.maximum(1, lens // 2))
+    args = dict(max_len=int(lens.max()), keep_last=1)
+
+    def step(total, idx):
+        rc.attend_weights(x.q, x.lse, x.rt.cu_q, x.rt.cu_ctx, 1, x.rt.cu_rows, x.rt.mask, uo, ur, 0, res_k=x.rk,
+                          res_w=total, res_w_prior=total)
+        rc.select_kept(total, x.rt.cu_rows, dev_kept, idx, **args)
+
+    dev_kept = i32(cu_kept)
+    ours, theirs = (torch.zeros(x.rk.shape[:-1], device=DEV) for _ in "ab")
+    a, b = (torch.zeros(int(cu_kept[-1]), dtype=torch.int32, device=DEV) for _ in "ab")
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step(ours, a)
+    for i in range(4):
+        x.q.normal_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            step(theirs, b)
+        torch.cuda.synchronize()
+        assert torch.equal(ours, theirs) and torch.equal(a, b), i
