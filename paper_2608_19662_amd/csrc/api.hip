@@ -804,7 +804,7 @@ int recache_attend_weights(int dtype, int layer, int n_layers, int n_req, const 
 
 size_t recache_select_workspace_bytes(int n_seg, int total, int max_len) {
     if (n_seg < 1 || total < 0 || max_len < 0) return 0;
-    return select_workspace_bytes(total, max_len);
+    return select_workspace_bytes(n_seg, total, max_len);
 }
 
 int recache_select_kept(int n_seg, const int32_t* cu, int total, int max_len, int n_planes,
@@ -819,11 +819,11 @@ int recache_select_kept(int n_seg, const int32_t* cu, int total, int max_len, in
             keep_first, keep_last);
     REQUIRE(cu && cu_kept && (total == 0 || w) && (total_kept == 0 || kept_idx), RECACHE_EINVAL,
             "null pointer argument");
-    const size_t need = select_workspace_bytes(total, max_len);
+    const size_t need = select_workspace_bytes(n_seg, total, max_len);
     REQUIRE(need == 0 || (workspace && workspace_bytes >= need), RECACHE_EWORKSPACE,
             "selection from segments of %d rows needs a %zu-byte workspace, got %zu", max_len, need,
             workspace ? workspace_bytes : 0);
-    REQUIRE(((uintptr_t)workspace & 3) == 0, RECACHE_EINVAL, "workspace is not 4-byte aligned");
+    REQUIRE(need == 0 || ((uintptr_t)workspace & 7) == 0, RECACHE_EINVAL, "workspace is not 8-byte aligned");
     if (total_kept == 0) return ok();
     SelectArgs a{};
     a.n_seg = n_seg;

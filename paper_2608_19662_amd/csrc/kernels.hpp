@@ -248,11 +248,10 @@ struct SelectArgs {
     int keep_first, keep_last, max_len;
     int32_t* kept_idx;
     float* kept_w;   // [n_planes][total_kept] or NULL
-    uint32_t* keys;  // long segments: scores in order-preserving form [total],
-                     // then the kept rows [total_kept]
+    uint32_t* keys;  // workspace of long segments, 8-byte aligned
 };
 hipError_t launch_select(const SelectArgs& a, hipStream_t stream);
-size_t select_workspace_bytes(long total, int max_len);
+size_t select_workspace_bytes(int n_seg, long total, int max_len);
 int decode_splits(int n_req, int n_kv_heads, int max_kv);
 // The most partials per query head, requests times splits, that a batch of
 // n_req requests or any smaller one makes (a program that sizes its workspace

@@ -136,6 +136,7 @@ ATTEND = dict(dtype=1, layer=0, n_layers=1, n_req=2, cu_q=FAKE, cu_ctx=FAKE, ctx
     ("recache_select_kept", SELECT, dict(idx=None), rc.EINVAL),
     ("recache_select_kept", SELECT, dict(total=300000, max_len=200000), rc.EWORKSPACE),
     ("recache_select_kept", SELECT, dict(total=300000, max_len=200000, ws=FAKE, nb=100), rc.EWORKSPACE),
+    ("recache_select_kept", SELECT, dict(total=300000, max_len=200000, ws=FAKE + 4, nb=1 << 30), rc.EINVAL),
     ("recache_quantize_kv", QUANT, dict(dtype=2), rc.EUNSUPPORTED),
     ("recache_quantize_kv", QUANT, dict(d=32), rc.EUNSUPPORTED),
     ("recache_quantize_kv", QUANT, dict(n_seg=0), rc.EINVAL),
@@ -184,7 +185,7 @@ def test_sizes():
     assert rc.quantized_blocks(64, 1) == 2
     assert rc.quantized_blocks(2 ** 31 - 1, 16384) == (2 ** 31 - 1) // 64 + 16384
     assert rc.select_workspace_bytes(4, 100000, 300) == 0
-    assert rc.select_workspace_bytes(4, 100000, 99000) >= 800000
+    assert rc.select_workspace_bytes(4, 100000, 99000) >= 400000
 
 
 def test_binding_refuses_host_tensors_and_wrong_shapes():
