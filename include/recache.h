@@ -524,7 +524,8 @@ int recache_select_kept(int n_seg, const int32_t* cu, int total, int max_len, in
  *   k, v: source element (plane p, row t, dim i) at p * plane_stride + t *
  *       row_stride + i (elements): a head-major cache (head_dim, rows * head_dim),
  *       a projection [rows][n_kv_heads][head_dim] (n_kv_heads * head_dim,
- *       head_dim), ...; 16-byte aligned, strides multiples of 16 bytes
+ *       head_dim), ...; 16-byte aligned, strides multiples of 16 bytes,
+ *       row_stride below 2^22 elements
  *   src_rows: rows of a plane of the source (those that cu_new or cu names)
  *   k8, v8[n_planes][rows][head_dim]; k_exp, v_exp[n_planes][blocks]
  * Rows and scales that no new row touches are left as they are.

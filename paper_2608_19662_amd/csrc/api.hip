@@ -863,6 +863,8 @@ int recache_quantize_kv(int dtype, int n_seg, const int32_t* cu, const int32_t* 
     REQUIRE(row_stride >= 0 && plane_stride >= 0 && row_stride % per16 == 0 && plane_stride % per16 == 0,
             RECACHE_EINVAL, "strides %lld, %lld (rows, planes) must be non-negative multiples of 16 bytes",
             (long long)row_stride, (long long)plane_stride);
+    REQUIRE(row_stride < (1 << 22), RECACHE_EUNSUPPORTED, "row_stride %lld is not below 2^22 elements",
+            (long long)row_stride);
     REQUIRE(((uintptr_t)k & 15) == 0 && ((uintptr_t)v & 15) == 0 && ((uintptr_t)k8 & 15) == 0 &&
                 ((uintptr_t)v8 & 15) == 0,
             RECACHE_EINVAL, "k, v, k8 and v8 must be 16-byte aligned");

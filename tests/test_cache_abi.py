@@ -147,6 +147,7 @@ ATTEND = dict(dtype=1, layer=0, n_layers=1, n_req=2, cu_q=FAKE, cu_ctx=FAKE, ctx
     ("recache_quantize_kv", QUANT, dict(ve=None), rc.EINVAL),
     ("recache_quantize_kv", QUANT, dict(rs=127), rc.EINVAL),
     ("recache_quantize_kv", QUANT, dict(ps=-128), rc.EINVAL),
+    ("recache_quantize_kv", QUANT, dict(rs=1 << 22), rc.EUNSUPPORTED),
     ("recache_quantize_kv", QUANT, dict(k=FAKE + 8), rc.EINVAL),
     ("recache_quantize_kv", QUANT, dict(v8=FAKE + 4), rc.EINVAL),
     ("recache_attend_quantized", ATTEND, dict(dtype=0), rc.EUNSUPPORTED),
