@@ -46,15 +46,22 @@
 // across the loop, so that the registers spilled around the last tiles stay
 // few.
 //
+// Caches in 8 bits (quant8.hpp; prefill only).  The same loop over bf16 tiles in LDS:
+// a thread fetches 16 bytes of codes of one row and its scale into registers
+// where the bf16 form starts its copy, and writes them to LDS as bf16 (exact) at
+// the tile's end, so that a code is converted once per block.
+//
 // Tiles never cross a resource boundary in encode, and the reduction order
 // depends only on local indices, so a resource's outputs are bit-identical
 // wherever it is packed and whatever its neighbours are.
 #include <algorithm>
+#include <type_traits>
 #include <utility>
 
 #include "attn_tile.hpp"
 #include "common.hpp"
 #include "kernels.hpp"
+#include "quant8.hpp"
 
 namespace rc {
 
@@ -109,6 +116,15 @@ struct Smem {
     int seg_row[ENCODE ? 2 : kMaxSeg];
     int scan[2 * NW];  // of the segment-length scan
 };
+template <bool ENCODE, int NW>
+struct Smem8 : Smem<ENCODE, NW> {
+    int seg_slot[kMaxSeg];  // first scale slot
+};
+
+template <typename Args>
+constexpr bool kIs8 = std::is_same<Args, Attn8Args>::value;
+__device__ __forceinline__ const AttnArgs& attn_args(const AttnArgs& x) { return x; }
+__device__ __forceinline__ const AttnArgs& attn_args(const Attn8Args& x) { return x.a; }
 
 __device__ __forceinline__ void wait_vm0() {
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0), expcnt / lgkmcnt unconstrained
@@ -116,12 +132,14 @@ __device__ __forceinline__ void wait_vm0() {
 
 // NW waves per block, each owning one (row block, query head) pair; two waves
 // per SIMD either way (two 4-wave blocks or one 8-wave block per CU).
-template <int HD, bool ENCODE, int NW>
-__global__ __launch_bounds__(NW * 64, 8 / NW) void attn_mfma_kernel(const AttnArgs a) {
+template <int HD, bool ENCODE, int NW, typename Args>
+__global__ __launch_bounds__(NW * 64, 8 / NW) void attn_mfma_kernel(const Args args) {
     using TL = Tile<HD, NW>;
+    constexpr bool Q8 = kIs8<Args>;
+    const AttnArgs& a = attn_args(args);
     constexpr int kThreads = NW * 64;
     constexpr int ROWB = TL::ROWB, TILEB = TL::TILEB;
-    __shared__ Smem<ENCODE, NW> sm;
+    __shared__ typename std::conditional<Q8, Smem8<ENCODE, NW>, Smem<ENCODE, NW>>::type sm;
     __shared__ __attribute__((aligned(16))) char k_st0[TILEB], k_st1[TILEB], v_st0[TILEB], v_st1[TILEB];
 
     const int tid = threadIdx.x;
@@ -176,6 +194,8 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void attn_mfma_kernel(const AttnAr
         q_len = a.cu_q[unit + 1] - q_row0;
         ctx_row0 = a.cu_ctx[unit];
         tc = a.cu_ctx[unit + 1] - ctx_row0;
+        if constexpr (Q8)
+            if (args.ctx_len) tc = args.ctx_len[unit];
     }
     // this wave's pair, and the rows of the block
     const int R = a.ratio;
@@ -206,6 +226,13 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void attn_mfma_kernel(const AttnAr
         }
         s_vis = segment_table<NW, false>(a.route_res + r0, n_seg, a.cu_kept, a.res_off, a.n_kv_heads, g, 0,
                                          sm.seg_start, sm.seg_row, sm.scan);
+        if constexpr (Q8) {
+            for (int s = tid; s < n_seg; s += kThreads) {
+                const int r = a.route_res[r0 + s];
+                sm.seg_slot[s] = (int)block_slot(sm.seg_row[s], a.res_off ? (long)r * a.n_kv_heads + g : r);
+            }
+            __syncthreads();
+        }
     }
     off = s_vis + tc - q_len;
     stream = s_vis + tc;
@@ -371,6 +398,84 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void attn_mfma_kernel(const AttnAr
         }
     };
 
+    // ---- 8-bit caches: HBM -> registers -> LDS.  Per wave RPW rows of a tile; a
+    // lane takes CB bytes of codes of a row, in NF fetches.
+    constexpr int CB = HD == 64 && NW == 8 ? 8 : 16;
+    constexpr int PPR = HD / CB, RPF = 64 / PPR, NF = TL::RPW / RPF;  // lanes per row, rows per fetch, fetches
+    struct Fetched {
+        u32x4 w[NF];
+        uint32_t e[NF];
+    };
+    // the tile set up last: row, slot and plane of this lane's fetches
+    int f_row[NF] = {}, f_slot[NF] = {};
+    uint32_t f_ctx = 0;
+    auto find_rows = [&](int kt) {
+        if constexpr (Q8) {
+            static_for<NF>([&](auto jc) {
+                constexpr int j = decltype(jc)::value;
+                const int p = min(kt * kBK + wave * TL::RPW + j * RPF + lane / PPR, stream - 1);
+                int beg, at, slot;
+                const bool ctx = p >= s_vis;
+                if (!ctx) {
+                    while (p >= seg_hi && sidx + 1 < n_seg) seg_hi = sm.seg_start[++sidx + 1];
+                    beg = sm.seg_row[sidx];
+                    at = p - sm.seg_start[sidx];
+                    slot = sm.seg_slot[sidx];
+                    f_ctx &= ~(1u << j);
+                } else {
+                    beg = ctx_row0;
+                    at = p - s_vis;
+                    slot = (int)block_slot(ctx_row0, unit);
+                    f_ctx |= 1u << j;
+                }
+                // in bounds whatever the tables hold
+                f_row[j] = max(0, min(beg + at, (int)(ctx ? a.c_rows : a.k_rows) - 1));
+                f_slot[j] = max(0, min(slot + at / kBlk8, (int)(ctx ? args.c_slots : args.r_slots) - 1));
+            });
+        }
+    };
+    auto fetch = [&](bool is_v, Fetched& f) {
+        if constexpr (Q8) {
+#pragma unroll
+            for (int j = 0; j < NF; ++j) {
+                const bool ctx = (f_ctx >> j) & 1;
+                const uint8_t* codes = ctx ? (is_v ? args.cv : args.ck) + (size_t)g * a.c_rows * HD
+                                           : (is_v ? args.rv : args.rk) + (size_t)g * a.k_gstride * HD;
+                const uint8_t* exps = ctx ? (is_v ? args.cv_exp : args.ck_exp) + (size_t)g * args.c_slots
+                                          : (is_v ? args.rv_exp : args.rk_exp) + (size_t)g * args.r_sstride;
+                const uint8_t* src = codes + (size_t)f_row[j] * HD + lane % PPR * CB;
+                if constexpr (CB == 16) {
+                    f.w[j] = *reinterpret_cast<const u32x4*>(src);
+                } else {
+                    const u32x2 w = *reinterpret_cast<const u32x2*>(src);
+                    f.w[j][0] = w[0], f.w[j][1] = w[1];
+                }
+                f.e[j] = exps[f_slot[j]];
+            }
+        }
+    };
+    auto put = [&](const Fetched& f, char* buf) {
+        if constexpr (Q8) {
+#pragma unroll
+            for (int j = 0; j < NF; ++j) {
+                const int row = wave * TL::RPW + j * RPF + lane / PPR;
+                const float scale = block_scale(f.e[j]);
+                if constexpr (CB == 16) {
+                    // a lane's two chunks in an order that differs between
+                    // neighbouring rows, whose even chunks share banks
+                    const int c = lane % PPR * 2, odd = row & 1;
+                    const u32x4 lo = codes_to_bf16x8(f.w[j][0], f.w[j][1], scale);
+                    const u32x4 hi = codes_to_bf16x8(f.w[j][2], f.w[j][3], scale);
+                    *reinterpret_cast<u32x4*>(buf + swz<HD>(row, c + odd)) = odd ? hi : lo;
+                    *reinterpret_cast<u32x4*>(buf + swz<HD>(row, c + 1 - odd)) = odd ? lo : hi;
+                } else {
+                    *reinterpret_cast<u32x4*>(buf + swz<HD>(row, lane % PPR)) =
+                        codes_to_bf16x8(f.w[j][0], f.w[j][1], scale);
+                }
+            }
+        }
+    };
+
     // Query rows first (they are needed first, for the RoPE), then the
     // prologue copies: K(0), V(0) into stage 0, K(1) into stage 1.  The
     // sources of tile 1 are kept for V(1) in the first loop iteration.
@@ -381,12 +486,27 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void attn_mfma_kernel(const AttnAr
         for (int t = 0; t < TL::NT; ++t)
             qraw[t] = *reinterpret_cast<const u32x4*>(qrow + t * 16 + half * 8);
     }
-    key_ptrs(0);
-    copy(false, k_st0);
-    copy(true, v_st0);
-    if (n_tiles > 1) {
-        key_ptrs(1);
-        copy(false, k_st1);
+    Fetched f_k, f_v;  // K(t + 2) and V(t + 1) of 8-bit caches
+    if constexpr (Q8) {
+        Fetched f_k0;
+        find_rows(0);
+        fetch(false, f_k0);
+        fetch(true, f_v);
+        if (n_tiles > 1) {
+            find_rows(1);
+            fetch(false, f_k);
+        }
+        put(f_k0, k_st0);
+        put(f_v, v_st0);
+        if (n_tiles > 1) put(f_k, k_st1);
+    } else {
+        key_ptrs(0);
+        copy(false, k_st0);
+        copy(true, v_st0);
+        if (n_tiles > 1) {
+            key_ptrs(1);
+            copy(false, k_st1);
+        }
     }
 
     // ---- Q fragment (B operand of S^T = K Q^T): lane holds row my_q, elements
@@ -513,10 +633,18 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void attn_mfma_kernel(const AttnAr
     auto tile = [&](auto stage_tag, auto next_tag, int kt) {
         constexpr int cur = decltype(stage_tag)::value;
         constexpr bool NEXT = decltype(next_tag)::value != 0;
-        if constexpr (NEXT) copy(true, cur ? v_st0 : v_st1);
-        if (kt + 2 < n_tiles) {
-            key_ptrs(kt + 2);
-            copy(false, cur ? k_st1 : k_st0);
+        if constexpr (Q8) {
+            if constexpr (NEXT) fetch(true, f_v);
+            if (kt + 2 < n_tiles) {
+                find_rows(kt + 2);
+                fetch(false, f_k);
+            }
+        } else {
+            if constexpr (NEXT) copy(true, cur ? v_st0 : v_st1);
+            if (kt + 2 < n_tiles) {
+                key_ptrs(kt + 2);
+                copy(false, cur ? k_st1 : k_st0);
+            }
         }
         f32x16* sc = sacc[cur];
         // causal / stream-end mask, only on tiles that reach past the first row's limit
@@ -620,7 +748,12 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void attn_mfma_kernel(const AttnAr
             }
         }
         if constexpr (NEXT) {
-            wait_vm0();
+            if constexpr (Q8) {
+                put(f_v, cur ? v_st0 : v_st1);
+                if (kt + 2 < n_tiles) put(f_k, cur ? k_st1 : k_st0);
+            } else {
+                wait_vm0();
+            }
             __syncthreads();  // V(t + 1), K(t + 2) in LDS; stage cur free again
         }
     };
@@ -688,17 +821,22 @@ namespace {
 // loop.
 constexpr int kEncodeWaves = 4;
 
-template <int HD, bool ENCODE, int NW>
-hipError_t launch(const AttnArgs& a, hipStream_t stream) {
-    AttnArgs b = a;
+AttnArgs& attn_args_of(AttnArgs& x) { return x; }
+AttnArgs& attn_args_of(Attn8Args& x) { return x.a; }
+
+template <int HD, bool ENCODE, int NW, typename Args>
+hipError_t launch(const Args& args, hipStream_t stream) {
+    Args copy = args;
+    AttnArgs& b = attn_args_of(copy);
+    const AttnArgs a = b;
     b.n_rb = (int)(((long)a.max_rows + 31) / 32);
     const long pairs = (long)b.n_rb * a.ratio;
     const long blocks = (pairs + NW - 1) / NW * b.n_units * b.n_kv_heads;
     if (blocks <= 0) return hipSuccess;
     if (blocks > 0x7fffffffL) return hipErrorInvalidValue;
     b.n_qt = (int)((pairs + NW - 1) / NW);
-    hipLaunchKernelGGL((attn_mfma_kernel<HD, ENCODE, NW>), dim3((unsigned)blocks), dim3(NW * 64), 0,
-                       stream, b);
+    hipLaunchKernelGGL((attn_mfma_kernel<HD, ENCODE, NW, Args>), dim3((unsigned)blocks), dim3(NW * 64), 0,
+                       stream, copy);
     return hipGetLastError();
 }
 
@@ -760,6 +898,17 @@ hipError_t launch_attn_mfma(const AttnArgs& a, bool encode, int head_dim, hipStr
     switch (prefill_form(a)) {
         case PrefillForm::kSplit8: return launch_attn_split(a, head_dim, 8, stream);
         case PrefillForm::kSplit4: return launch_attn_split(a, head_dim, 4, stream);
+        case PrefillForm::kBlocks4:
+            return head_dim == 128 ? launch<128, false, 4>(a, stream) : launch<64, false, 4>(a, stream);
+        default: return head_dim == 128 ? launch<128, false, 8>(a, stream) : launch<64, false, 8>(a, stream);
+    }
+}
+
+hipError_t launch_attn8(const Attn8Args& a, int head_dim, hipStream_t stream) {
+    if (a.a.ratio < 1 || a.a.max_rows < 1) return hipErrorInvalidValue;
+    switch (prefill_form(a.a)) {
+        case PrefillForm::kSplit8: return launch_attn_split8(a, head_dim, 8, stream);
+        case PrefillForm::kSplit4: return launch_attn_split8(a, head_dim, 4, stream);
         case PrefillForm::kBlocks4:
             return head_dim == 128 ? launch<128, false, 4>(a, stream) : launch<64, false, 4>(a, stream);
         default: return head_dim == 128 ? launch<128, false, 8>(a, stream) : launch<64, false, 8>(a, stream);

@@ -419,10 +419,4 @@ hipError_t launch_attn_split8(const Attn8Args& a, int head_dim, int waves, hipSt
     return waves == 8 ? launch<64, 8>(b, grid.compact, n, stream) : launch<64, 4>(b, grid.compact, n, stream);
 }
 
-hipError_t launch_attn8(const Attn8Args& a, int head_dim, hipStream_t stream) {
-    if (a.a.ratio < 1 || a.a.max_rows < 1) return hipErrorInvalidValue;
-    const long col_blocks = std::max((a.a.lse_rows * a.a.ratio + 31) / 32, (long)a.a.n_units) * a.a.n_kv_heads;
-    return launch_attn_split8(a, head_dim, col_blocks <= 256 ? 8 : 4, stream);
-}
-
 }  // namespace rc
