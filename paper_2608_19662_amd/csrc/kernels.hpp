@@ -231,6 +231,7 @@ struct WeighArgs {
     const int32_t* user_off;
     const int32_t* user_req;
     int n_users;
+    uint32_t inv_ratio;     // the launcher's: 65536 / ratio + 1
     long r_items, c_items;  // the launcher's: bounds on key tiles, of a plane (of all with res_off)
 };
 hipError_t launch_weigh(const WeighArgs& a, int elem_bytes, int head_dim, hipStream_t stream);

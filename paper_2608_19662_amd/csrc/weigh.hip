@@ -15,7 +15,9 @@
 //                                 queries stays in the lanes until the end
 // Its waves take the column tiles in turn.
 #include <algorithm>
+#include <type_traits>
 
+#include "attn_tile.hpp"
 #include "common.hpp"
 #include "kernels.hpp"
 
@@ -87,6 +89,73 @@ __device__ __forceinline__ float lane_totals(const float* v, int lane) {
     }
 }
 
+// A block's keys: a tile of KT rows of a resource or of a context.
+struct KeyTile {
+    bool ctx;
+    int g, u0, u1;  // plane, and the segment's users: user_req[u0 .. u1), or request u0 itself
+    size_t row0;    // first key row, planes counted through
+    int n;          // keys (0: nothing to do)
+    int off;        // context: query i sees keys up to off + i of the tile
+    template <int KT>
+    __device__ __forceinline__ void locate(const WeighArgs& a, int lane) {
+        const int G = a.n_kv_heads;
+        long bid = blockIdx.x;
+        const long n_r = a.r_w ? (a.res_off ? a.r_items : a.r_items * G) : 0;
+        ctx = bid >= n_r;
+        off = 0;
+        long beg, len, j;
+        if (!ctx) {
+            int r;
+            if (a.res_off) {
+                const int s = find_segment(a.res_off, a.n_res * G, KT, 1, bid, lane);
+                r = s / G;
+                g = s % G;
+                beg = a.res_off[s];
+                j = bid - first_item(beg, s, KT, 1);
+            } else {
+                g = (int)(bid % G);
+                bid /= G;
+                r = find_segment(a.cu_kept, a.n_res, KT, 1, bid, lane);
+                beg = a.cu_kept[r];
+                j = bid - first_item(beg, r, KT, 1);
+            }
+            len = (long)a.cu_kept[r + 1] - a.cu_kept[r];
+            const bool seen = a.mask[((size_t)r * a.n_layers + a.layer) * G + g] != 0;
+            if (a.res_off && !seen) len = 0;  // (a route that the store does not hold)
+            u0 = seen ? max(a.user_off[r], 0) : 0;
+            u1 = seen ? min(a.user_off[r + 1], a.n_users) : 0;
+        } else {
+            bid -= n_r;
+            g = (int)(bid % G);
+            bid /= G;
+            const int b = find_segment(a.cu_ctx, a.n_req, KT, 1, bid, lane);
+            beg = a.cu_ctx[b];
+            len = a.cu_ctx[b + 1] - beg;
+            j = bid - first_item(beg, b, KT, 1);
+            off = (int)(len - (a.cu_q[b + 1] - a.cu_q[b]) - j * KT);
+            u0 = b;
+            u1 = b + 1;
+        }
+        const long rows = ctx ? a.c_rows : a.r_rows, first = beg + j * KT;
+        // in bounds whatever the offsets hold
+        n = j < 0 || first < 0 ? 0 : (int)max(0L, min(min((long)KT, len - j * KT), rows - first));
+        row0 = (ctx || !a.res_off ? (size_t)g * rows : 0) + first;
+    }
+    __device__ __forceinline__ int user(const WeighArgs& a, int u) const {
+        return ctx ? u : max(0, min(a.user_req[u], a.n_req - 1));
+    }
+    // Key i's sum joins its prior.
+    __device__ __forceinline__ void write(const WeighArgs& a, int i, float sum) const {
+        const float* prior = ctx ? a.c_prior : a.r_prior;
+        (ctx ? a.c_w : a.r_w)[row0 + i] = (prior ? prior[row0 + i] : 0.f) + sum;
+    }
+};
+
+// The key of value v of a lane (lane_totals) among its 32-key blocks.
+__device__ __forceinline__ int key_of_value(int v, int half) {
+    return (v >> 4) * 32 + ((v & 15) >> 2) * 8 + half * 4 + (v & 3);
+}
+
 template <typename T, int HD, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void weigh_kernel(const WeighArgs a) {
     constexpr int NKB = Frag<T, HD>::kBlocks, KT = 32 * NKB;
@@ -94,62 +163,16 @@ __global__ __launch_bounds__(NW * 64, 2) void weigh_kernel(const WeighArgs a) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, half = lane >> 5;
-    const int R = a.ratio, G = a.n_kv_heads;
-
-    // ---- this block's keys: tile j of a resource's rows or of a context
-    long bid = blockIdx.x;
-    const long n_r = a.r_w ? (a.res_off ? a.r_items : a.r_items * G) : 0;
-    const bool ctx = bid >= n_r;
-    int g, u0, u1;   // plane, and the users of the segment: user_req[u0 .. u1), or request u0 itself
-    long row0;       // first key row
-    int n;           // keys
-    int off = 0;     // context: query i sees keys up to off + i of the tile
-    if (!ctx) {
-        int r;
-        long j, beg;
-        if (a.res_off) {
-            const int s = find_segment(a.res_off, a.n_res * G, KT, 1, bid, lane);
-            r = s / G;
-            g = s % G;
-            beg = a.res_off[s];
-            j = bid - first_item(beg, s, KT, 1);
-        } else {
-            g = (int)(bid % G);
-            bid /= G;
-            r = find_segment(a.cu_kept, a.n_res, KT, 1, bid, lane);
-            beg = a.cu_kept[r];
-            j = bid - first_item(beg, r, KT, 1);
-        }
-        long len = (long)a.cu_kept[r + 1] - a.cu_kept[r];
-        const bool seen = a.mask[((size_t)r * a.n_layers + a.layer) * G + g] != 0;
-        if (a.res_off && !seen) len = 0;  // (a route that the store does not hold)
-        row0 = beg + j * KT;
-        n = j < 0 ? 0 : (int)max(0L, min((long)KT, len - j * KT));
-        u0 = seen ? max(a.user_off[r], 0) : 0;
-        u1 = seen ? min(a.user_off[r + 1], a.n_users) : 0;
-    } else {
-        bid -= n_r;
-        g = (int)(bid % G);
-        bid /= G;
-        const int b = find_segment(a.cu_ctx, a.n_req, KT, 1, bid, lane);
-        const long beg = a.cu_ctx[b], len = a.cu_ctx[b + 1] - beg;
-        const long j = bid - first_item(beg, b, KT, 1);
-        row0 = beg + j * KT;
-        n = j < 0 ? 0 : (int)max(0L, min((long)KT, len - j * KT));
-        off = (int)(len - (a.cu_q[b + 1] - a.cu_q[b]) - j * KT);
-        u0 = b;
-        u1 = b + 1;
-    }
-    const long rows = ctx ? a.c_rows : a.r_rows;
-    if (row0 < 0) n = 0;
-    n = (int)min((long)n, max(rows - row0, 0L));  // in bounds whatever the offsets hold
-    if (n <= 0) return;
-    const size_t plane = (ctx || !a.res_off) ? (size_t)g * rows : 0;
+    const int R = a.ratio;
+    KeyTile t;
+    t.locate<KT>(a, lane);
+    if (t.n <= 0) return;
+    const int g = t.g, off = t.off;
 
     Frag<T, HD> kf[NKB];
 #pragma unroll
     for (int kb = 0; kb < NKB; ++kb)
-        kf[kb].load(static_cast<const T*>(ctx ? a.ck : a.rk) + (plane + row0 + min(kb * 32 + l32, n - 1)) * HD, half);
+        kf[kb].load(static_cast<const T*>(t.ctx ? a.ck : a.rk) + (t.row0 + min(kb * 32 + l32, t.n - 1)) * HD, half);
 
     float acc[NKB * 16] = {};
     // One tile of columns: this lane's query row and head, and from which key
@@ -173,26 +196,26 @@ __global__ __launch_bounds__(NW * 64, 2) void weigh_kernel(const WeighArgs a) {
             for (int r = 0; r < 16; ++r) acc[kb * 16 + r] += __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2, -lse2));
         }
     };
-    if (a.one_query && !ctx) {
+    if (a.one_query && !t.ctx) {
         // one query per request: columns run over the users
-        const int n_cols = (u1 - u0) * R;
+        const int n_cols = (t.u1 - t.u0) * R;
         for (int j0 = wave * 32; j0 < n_cols; j0 += NW * 32) {
             const int j = min(j0 + l32, n_cols - 1);
-            const int b = max(0, min(a.user_req[u0 + j / R], a.n_req - 1));
+            const int b = t.user(a, t.u0 + j / R);
             const int q0 = a.cu_q[b];
             columns(q0, g * R + j % R, j0 + l32 < n_cols, KT, a.cu_q[b + 1] - q0 != 1);
         }
     } else {
         int turn = 0;  // column tiles so far, modulo the waves
-        for (int u = u0; u < u1; ++u) {
-            const int b = ctx ? u : max(0, min(a.user_req[u], a.n_req - 1));
+        for (int u = t.u0; u < t.u1; ++u) {
+            const int b = t.user(a, u);
             const int q0 = a.cu_q[b], n_cols = (a.cu_q[b + 1] - q0) * R;
             // context: rows before -off see none of these keys
-            const int first = ctx ? max(0, -off) * R / 32 * 32 : 0;
+            const int first = t.ctx ? max(0, -off) * R / 32 * 32 : 0;
             for (int j0 = first; j0 < n_cols; j0 += 32) {
                 if (turn == wave) {
                     const int j = min(j0 + l32, n_cols - 1);
-                    columns((long)q0 + j / R, g * R + j % R, j0 + l32 < n_cols, ctx ? off + j / R : KT, false);
+                    columns((long)q0 + j / R, g * R + j % R, j0 + l32 < n_cols, t.ctx ? off + j / R : KT, false);
                 }
                 turn = turn + 1 == NW ? 0 : turn + 1;
             }
@@ -201,18 +224,214 @@ __global__ __launch_bounds__(NW * 64, 2) void weigh_kernel(const WeighArgs a) {
 
     // ---- the sums of the lanes, then of the waves
     const float total = lane_totals<NKB * 16>(acc, lane);
-    const int v = NKB == 2 ? l32 : l32 >> 1;  // value of this lane: block v / 16, register v % 16
-    const int key = (v >> 4) * 32 + ((v & 15) >> 2) * 8 + half * 4 + (v & 3);
-    if (NKB == 2 || !(l32 & 1)) part[wave][key] = total;
+    const int v = NKB == 2 ? l32 : l32 >> 1;
+    if (NKB == 2 || !(l32 & 1)) part[wave][key_of_value(v, half)] = total;
     __syncthreads();
-    if (tid < n) {
-        float* w = ctx ? a.c_w : a.r_w;
-        const float* prior = ctx ? a.c_prior : a.r_prior;
+    if (tid < t.n) {
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < NW; ++i) sum += part[i][tid];
-        w[plane + row0 + tid] = (prior ? prior[plane + row0 + tid] : 0.f) + sum;
+        t.write(a, tid, sum);
     }
+}
+
+// The same for prompts in bf16, where products and exponentials count: a block
+// owns 128 keys and takes the columns 128 at a time through LDS; its waves are two
+// halves of the keys by two of the columns, which each takes as two tiles of 32.  A
+// tile is 16 MFMAs and 32 exponentials per lane, each with an fma and an add: about
+// the same time on the matrix pipe and the VALU.  So the products of a tile run
+// beside the exponentials of the one before it, those of the two key blocks in turn (a
+// product waits for the one before it in the same accumulator).
+template <int HD>
+__global__ __launch_bounds__(256, 2) void weigh_prompt_kernel(const WeighArgs a) {
+    constexpr int KT = 128, CT = 128, CW = CT / 2;  // keys, columns, a wave's columns
+    constexpr int CPR = HD / 8, ROWB = HD * 2;  // 16-byte chunks, bytes per row
+    constexpr int RPI = 64 / CPR;               // columns per 1 KB copy
+    constexpr int NJ = CT / 4 / RPI;            // copies per wave and step
+    constexpr int NT = HD / 16;                 // MFMA steps
+    // (two arrays: the compiler then sees that copies in flight into one do not
+    // touch the columns being read)
+    __shared__ __attribute__((aligned(16))) char q_st0[CT * ROWB], q_st1[CT * ROWB];
+    __shared__ float part[2][KT];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, half = lane >> 5;
+    const int kh = wave & 1, ch = wave >> 1;
+    const int R = a.ratio;
+    KeyTile t;
+    t.locate<KT>(a, lane);
+    if (t.n <= 0) return;
+    const int g = __builtin_amdgcn_readfirstlane(t.g);
+    t.off = __builtin_amdgcn_readfirstlane(t.off);
+    t.u0 = __builtin_amdgcn_readfirstlane(t.u0);
+    t.u1 = __builtin_amdgcn_readfirstlane(t.u1);
+
+    Frag<uint16_t, HD> kf[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+        kf[kb].load(static_cast<const uint16_t*>(t.ctx ? a.ck : a.rk) +
+                        (t.row0 + min(kh * 64 + kb * 32 + l32, t.n - 1)) * HD,
+                    half);
+
+    // ---- the steps: CT columns (row, head) of a user, rows first
+    struct Step {
+        int u, q0, n_rows, n_cols, j0;  // (u past the users: none)
+        int row0, rem;                  // j0 / R and j0 % R
+    };
+    const int step_rows = CT / R, step_rem = CT - step_rows * R;
+    auto open = [&](Step& s) {  // the first step of user s.u or of the first after it that has one
+        for (; s.u < t.u1; ++s.u) {
+            const int b = __builtin_amdgcn_readfirstlane(t.user(a, s.u));
+            s.q0 = __builtin_amdgcn_readfirstlane(a.cu_q[b]);
+            s.n_rows = max(0, min(__builtin_amdgcn_readfirstlane(a.cu_q[b + 1]) - s.q0, (int)a.total_q - s.q0));
+            if (s.q0 < 0) s.n_rows = 0;
+            s.n_cols = s.n_rows * R;
+            // context: rows before -off see none of these keys
+            s.row0 = t.ctx ? max(0, -t.off) : 0;
+            s.j0 = s.row0 * R;
+            s.rem = 0;
+            if (s.j0 < s.n_cols) return;
+        }
+    };
+    auto advance = [&](Step& s) {
+        s.j0 += CT;
+        s.row0 += step_rows;
+        s.rem += step_rem;
+        if (s.rem >= R) s.rem -= R, ++s.row0;
+        if (s.j0 >= s.n_cols) {
+            ++s.u;
+            open(s);
+        }
+    };
+    auto uniform = [](const void* p) {
+        const uint64_t u = (uint64_t)p;
+        return (void*)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32) |
+                       (uint32_t)__builtin_amdgcn_readfirstlane((int)u));
+    };
+    // c / R of a column c < CT + 8 from a row's first
+    auto row_of = [&](int c) { return (int)(__umul24((uint32_t)c, a.inv_ratio) >> 16); };
+    // Copies of a step's query rows, by the swizzle of the key tiles of prefill:
+    // copy j of a wave moves columns wave*CT/4 + j*RPI + [0, RPI); lane i lands at byte
+    // 16 i, chunk i % CPR of its column.  Columns past the last are zeros.  Where
+    // R divides CT every step starts at a row, and a lane's offsets stay.
+    int offsets[NJ];
+    auto find_offsets = [&](int rem) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            const int col = wave * (CT / 4) + j * RPI + lane / CPR, c = rem + col;
+            const int at = row_of(c) * (a.n_q_heads - R) + c;  // in heads from row0's first
+            offsets[j] = at * ROWB + (((lane % CPR) ^ chunk_mask<CPR>(col)) << 4);
+        }
+    };
+    find_offsets(0);
+    auto copy = [&](const Step& s, char* dst) {
+        if (step_rem) find_offsets(s.rem);
+        const int rows = min(s.n_rows - s.row0, CT);  // (CT columns span no more)
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+            uniform(static_cast<const uint16_t*>(a.q) + ((size_t)(s.q0 + s.row0) * a.n_q_heads + g * R) * HD), (short)0,
+            __builtin_amdgcn_readfirstlane(((rows - 1) * a.n_q_heads + R) * ROWB), kBufferFlags);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(dst + (wave * (CT / 4) + j * RPI) * ROWB), 16,
+                                                     (int)offsets[j], 0, 0, 0);
+    };
+    // This lane's columns of a step, one of each tile: their log-sum-exps (past the
+    // last column: some other one's) and the last keys of the wave's that they see.
+    struct Columns {
+        float lse[2];
+        int last[2];
+    };
+    auto columns = [&](const Step& s) {
+        Columns x;
+        const float* p = a.lse + (size_t)g * R * a.total_q + s.q0 + s.row0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int c = s.rem + min(ch * CW + i * 32 + l32, s.n_cols - s.j0 - 1), row = row_of(c);
+            x.lse[i] = p[(size_t)(c - row * R) * a.total_q + row];
+            x.last[i] = t.ctx ? t.off + s.row0 + row - kh * 64 : KT;
+        }
+        return x;
+    };
+
+    float acc[32] = {};
+    const float sl2 = a.scale_log2;
+    const uint32_t q_rd = (uint32_t)(ch * CW * ROWB) + swz<HD>(l32, half);  // (the mask repeats after 16 rows)
+    Step s{t.u0, 0, 0, 0, 0, 0, 0}, next;
+    open(s);
+    if (s.u < t.u1) {
+        copy(s, q_st0);
+        f32x16 x[2][2] = {};  // logits of a step's tiles, of the wave's two key blocks
+        float lse_prev = INFINITY;  // of the tile whose exponentials are due, in units of log2(e)
+        Columns col = columns(s);
+        auto step = [&](auto stage) {
+            constexpr int cur = decltype(stage)::value;
+            __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+            __syncthreads();  // this step's columns are in LDS, the other stage is read
+            // (+inf past the last column: weighs nothing)
+            float lse2[2];
+            int last[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                lse2[i] = s.j0 + ch * CW + i * 32 + l32 < s.n_cols ? col.lse[i] * kLog2e : INFINITY;
+                last[i] = col.last[i];
+            }
+            next = s;
+            advance(next);
+            const bool more = next.u < t.u1;
+            if (more) {
+                copy(next, cur ? q_st0 : q_st1);
+                col = columns(next);
+            }
+            const char* st = cur ? q_st1 : q_st0;
+#pragma unroll
+            for (int tile = 0; tile < 2; ++tile) {
+                f32x16* now = x[tile];
+                now[0] = now[1] = f32x16{};
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    const bf16x8 q =
+                        *reinterpret_cast<const bf16x8*>(st + tile * 32 * ROWB + (q_rd ^ (uint32_t)(i << 5)));
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb)
+                        now[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[kb].w[i]), q,
+                                                                          now[kb], 0, 0, 0);
+                }
+#pragma unroll
+                for (int r = 0; r < 32; ++r)
+                    acc[r] += __builtin_amdgcn_exp2f(fmaf(x[tile ^ 1][r >> 4][r & 15], sl2, -lse_prev));
+                // two reads ahead, then every product with its share of 32 fma, exp and add
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+                for (int i = 0; i < 2 * NT; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x402, 96 / (2 * NT), 0);
+                    if (i % 2 == 1 && i / 2 + 2 < NT) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                // (without this the sums sink below the branch, away from the products)
+#pragma unroll
+                for (int r = 0; r < 32; ++r) asm volatile("" : "+v"(acc[r]));
+                if (__builtin_amdgcn_ballot_w64(last[tile] < 63) != 0) {
+#pragma unroll
+                    for (int r = 0; r < 32; ++r)
+                        if ((r >> 4) * 32 + ((r & 15) >> 2) * 8 + half * 4 + (r & 3) > last[tile])
+                            now[r >> 4][r & 15] = -INFINITY;
+                }
+                lse_prev = lse2[tile];
+            }
+            s = next;
+            return more;
+        };
+        while (step(std::integral_constant<int, 0>{}) && step(std::integral_constant<int, 1>{})) {
+        }
+#pragma unroll
+        for (int r = 0; r < 32; ++r) acc[r] += __builtin_amdgcn_exp2f(fmaf(x[1][r >> 4][r & 15], sl2, -lse_prev));
+    }
+    const float total = lane_totals<32>(acc, lane);
+    part[ch][kh * 64 + key_of_value(l32, half)] = total;
+    __syncthreads();
+    if (tid < t.n) t.write(a, tid, part[0][tid] + part[1][tid]);
 }
 
 // One wave per resource: its users are the list entries that name it, in
@@ -246,26 +465,36 @@ __global__ __launch_bounds__(256) void users_kernel(int n_req, const int32_t* re
     }
 }
 
+// Blocks of a grid of KT-key tiles; fills the item counts.
+long key_blocks(WeighArgs& a, int kt) {
+    a.r_items = a.res_off ? a.r_rows / kt + (long)a.n_res * a.n_kv_heads : a.r_rows / kt + a.n_res;
+    a.c_items = a.c_rows / kt + a.n_req;
+    return (a.r_w ? (a.res_off ? a.r_items : a.r_items * a.n_kv_heads) : 0) + (a.c_w ? a.c_items * a.n_kv_heads : 0);
+}
+
 template <typename T, int HD>
 hipError_t launch(const WeighArgs& b, hipStream_t stream) {
     WeighArgs a = b;
-    constexpr int KT = 32 * Frag<T, HD>::kBlocks;
-    a.r_items = a.res_off ? a.r_rows / KT + (long)a.n_res * a.n_kv_heads : a.r_rows / KT + a.n_res;
-    a.c_items = a.c_rows / KT + a.n_req;
-    const long blocks = (a.r_w ? (a.res_off ? a.r_items : a.r_items * a.n_kv_heads) : 0) +
-                        (a.c_w ? a.c_items * a.n_kv_heads : 0);
+    const bool prompt = sizeof(T) == 2 && !a.one_query;
+    const long blocks = key_blocks(a, prompt ? 128 : 32 * Frag<T, HD>::kBlocks);
     if (blocks <= 0) return hipSuccess;
     if (blocks > 0x7fffffffL) return hipErrorInvalidValue;
-    if (a.one_query)
-        hipLaunchKernelGGL((weigh_kernel<T, HD, 1>), dim3((unsigned)blocks), dim3(64), 0, stream, a);
-    else
-        hipLaunchKernelGGL((weigh_kernel<T, HD, 4>), dim3((unsigned)blocks), dim3(256), 0, stream, a);
+    const dim3 grid((unsigned)blocks);
+    if (prompt)
+        hipLaunchKernelGGL(weigh_prompt_kernel<HD>, grid, dim3(256), 0, stream, a);
+    else if (a.one_query)
+        hipLaunchKernelGGL((weigh_kernel<T, HD, 1>), grid, dim3(64), 0, stream, a);
+    else if constexpr (sizeof(T) == 4)
+        hipLaunchKernelGGL((weigh_kernel<T, HD, 4>), grid, dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_weigh(const WeighArgs& a, int elem_bytes, int head_dim, hipStream_t stream) {
+hipError_t launch_weigh(const WeighArgs& b, int elem_bytes, int head_dim, hipStream_t stream) {
+    WeighArgs a = b;
+    if (a.ratio < 1) return hipErrorInvalidValue;
+    a.inv_ratio = 65536u / (uint32_t)a.ratio + 1;
     if (elem_bytes == 4) return head_dim == 128 ? launch<float, 128>(a, stream) : launch<float, 64>(a, stream);
     return head_dim == 128 ? launch<uint16_t, 128>(a, stream) : launch<uint16_t, 64>(a, stream);
 }
