@@ -7,13 +7,13 @@
 // taken: each probability is formed again from the row's log-sum-exp.
 //
 // Work is split by keys, so that no two blocks add to one sum and its order is
-// fixed: a block owns 64 rows of one segment and plane (32 in fp32), holds them
-// as the A operand of its MFMAs for its whole life, and walks the queries that
-// see them in order of the requests, 32 (row, head) columns at a time:
+// fixed: a block owns some rows of one segment and plane, holds them as the A
+// operand of its MFMAs for its whole life, and walks the queries that see them in
+// order of the requests, 32 (row, head) columns at a time:
 //     S = K Q^T (32x32 MFMA)      column c of every lane is one query, so that
 //     w += exp2(S - lse)          the log-sum-exp is one register and the sum over
 //                                 queries stays in the lanes until the end
-// Its waves take the column tiles in turn.
+// Three kernels: fp32, decode and prompts in bf16.
 #include <algorithm>
 #include <type_traits>
 
@@ -34,24 +34,14 @@ template <typename T, int HD>
 struct Frag;
 template <int HD>
 struct Frag<uint16_t, HD> {
-    static constexpr int kBlocks = 2;  // 32-key blocks per wave
     u32x4 w[HD / 16];
     __device__ __forceinline__ void load(const uint16_t* row, int half) {
 #pragma unroll
         for (int t = 0; t < HD / 16; ++t) w[t] = *reinterpret_cast<const u32x4*>(row + t * 16 + half * 8);
     }
-    static __device__ __forceinline__ f32x16 product(const Frag& a, const Frag& b) {
-        f32x16 c = {};
-#pragma unroll
-        for (int t = 0; t < HD / 16; ++t)
-            c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a.w[t]),
-                                                        __builtin_bit_cast(bf16x8, b.w[t]), c, 0, 0, 0);
-        return c;
-    }
 };
 template <int HD>
 struct Frag<float, HD> {
-    static constexpr int kBlocks = 1;
     f32x4 w[HD / 8];
     __device__ __forceinline__ void load(const float* row, int half) {
 #pragma unroll
@@ -144,21 +134,33 @@ struct KeyTile {
     __device__ __forceinline__ int user(const WeighArgs& a, int u) const {
         return ctx ? u : max(0, min(a.user_req[u], a.n_req - 1));
     }
+    __device__ __forceinline__ float prior(const WeighArgs& a, int i) const {
+        const float* p = ctx ? a.c_prior : a.r_prior;
+        return p ? p[row0 + i] : 0.f;
+    }
     // Key i's sum joins its prior.
     __device__ __forceinline__ void write(const WeighArgs& a, int i, float sum) const {
-        const float* prior = ctx ? a.c_prior : a.r_prior;
-        (ctx ? a.c_w : a.r_w)[row0 + i] = (prior ? prior[row0 + i] : 0.f) + sum;
+        (ctx ? a.c_w : a.r_w)[row0 + i] = prior(a, i) + sum;
     }
 };
+
+// A wave-uniform pointer, pinned to scalar registers.
+__device__ __forceinline__ void* uniform_ptr(const void* p) {
+    const uint64_t u = (uint64_t)p;
+    return (void*)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32) |
+                   (uint32_t)__builtin_amdgcn_readfirstlane((int)u));
+}
 
 // The key of value v of a lane (lane_totals) among its 32-key blocks.
 __device__ __forceinline__ int key_of_value(int v, int half) {
     return (v >> 4) * 32 + ((v & 15) >> 2) * 8 + half * 4 + (v & 3);
 }
 
-template <typename T, int HD, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void weigh_kernel(const WeighArgs a) {
-    constexpr int NKB = Frag<T, HD>::kBlocks, KT = 32 * NKB;
+// fp32: 32 keys per block, its waves take the column tiles in turn.
+template <int HD, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void weigh_f32_kernel(const WeighArgs a) {
+    constexpr int KT = 32;
+    typedef Frag<float, HD> F;
     __shared__ float part[NW][KT];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -169,32 +171,25 @@ __global__ __launch_bounds__(NW * 64, 2) void weigh_kernel(const WeighArgs a) {
     if (t.n <= 0) return;
     const int g = t.g, off = t.off;
 
-    Frag<T, HD> kf[NKB];
-#pragma unroll
-    for (int kb = 0; kb < NKB; ++kb)
-        kf[kb].load(static_cast<const T*>(t.ctx ? a.ck : a.rk) + (t.row0 + min(kb * 32 + l32, t.n - 1)) * HD, half);
-
-    float acc[NKB * 16] = {};
+    F kf;
+    kf.load(static_cast<const float*>(t.ctx ? a.ck : a.rk) + (t.row0 + min(l32, t.n - 1)) * HD, half);
+    float acc[16] = {};
     // One tile of columns: this lane's query row and head, and from which key
     // offset on it sees none (KT or more: sees all); used: the column counts.
     auto columns = [&](long row, int head, bool used, int last, bool wrong) {
         row = max(0L, min(row, a.total_q - 1));
-        Frag<T, HD> qf;
-        qf.load(static_cast<const T*>(a.q) + ((size_t)row * a.n_q_heads + head) * HD, half);
+        F qf;
+        qf.load(static_cast<const float*>(a.q) + ((size_t)row * a.n_q_heads + head) * HD, half);
         float lse2 = used ? a.lse[(size_t)head * a.total_q + row] * kLog2e : INFINITY;
         if (wrong) lse2 = __builtin_nanf("");  // (a caller's size error shows)
-        const bool diag = __builtin_amdgcn_ballot_w64(last < KT - 1) != 0;
+        f32x16 s = F::product(kf, qf);
+        if (__builtin_amdgcn_ballot_w64(last < KT - 1) != 0) {
 #pragma unroll
-        for (int kb = 0; kb < NKB; ++kb) {
-            f32x16 s = Frag<T, HD>::product(kf[kb], qf);
-            if (diag) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (kb * 32 + (r >> 2) * 8 + half * 4 + (r & 3) > last) s[r] = -INFINITY;
-            }
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[kb * 16 + r] += __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2, -lse2));
+            for (int r = 0; r < 16; ++r)
+                if ((r >> 2) * 8 + half * 4 + (r & 3) > last) s[r] = -INFINITY;
         }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[r] += __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2, -lse2));
     };
     if (a.one_query && !t.ctx) {
         // one query per request: columns run over the users
@@ -223,9 +218,8 @@ __global__ __launch_bounds__(NW * 64, 2) void weigh_kernel(const WeighArgs a) {
     }
 
     // ---- the sums of the lanes, then of the waves
-    const float total = lane_totals<NKB * 16>(acc, lane);
-    const int v = NKB == 2 ? l32 : l32 >> 1;
-    if (NKB == 2 || !(l32 & 1)) part[wave][key_of_value(v, half)] = total;
+    const float total = lane_totals<16>(acc, lane);
+    if (!(l32 & 1)) part[wave][key_of_value(l32 >> 1, half)] = total;
     __syncthreads();
     if (tid < t.n) {
         float sum = 0.f;
@@ -233,6 +227,67 @@ __global__ __launch_bounds__(NW * 64, 2) void weigh_kernel(const WeighArgs a) {
         for (int i = 0; i < NW; ++i) sum += part[i][tid];
         t.write(a, tid, sum);
     }
+}
+
+// The same for decode in bf16 (one query per request), where reading the keys
+// counts: a wave of its own for every 32 keys, which go into LDS in whole lines, so that
+// 20 waves per CU are on their way to memory, its segment and its queries at once.
+// 64 requests of 4,096 context rows and 32 of 256 resources each, 32 / 8 heads,
+// 597 MB: 115 us, 5.2 TB/s; 123 with 64 keys per wave (half as many waves), 154 with
+// those loaded as MFMA operands, 32 bytes of every row per instruction; runs of several
+// tiles per wave, the next one's rows in flight, lose as well.
+template <int HD>
+__global__ __launch_bounds__(64) void weigh_decode_kernel(const WeighArgs a) {
+    constexpr int KT = 32, CPR = HD / 8, ROWB = HD * 2, RPI = 64 / CPR, NT = HD / 16;
+    __shared__ __attribute__((aligned(16))) char k_st[KT * ROWB];
+    const int lane = threadIdx.x, l32 = lane & 31, half = lane >> 5;
+    const int R = a.ratio;
+    KeyTile t;
+    t.locate<KT>(a, lane);
+    if (t.n <= 0) return;
+    {
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+            uniform_ptr(static_cast<const uint16_t*>(t.ctx ? a.ck : a.rk) + t.row0 * HD), (short)0,
+            __builtin_amdgcn_readfirstlane(t.n * ROWB), kBufferFlags);
+#pragma unroll
+        for (int j = 0; j < KT / RPI; ++j) {
+            const int row = j * RPI + lane / CPR;  // (rows past the last are zeros)
+            const int o = row * ROWB + (((lane % CPR) ^ chunk_mask<CPR>(row)) << 4);
+            // (no request reads another's context)
+            if (t.ctx)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(k_st + j * 1024), 16, (int)o, 0, 0, 2);
+            else
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(k_st + j * 1024), 16, (int)o, 0, 0, 0);
+        }
+    }
+    const int key = key_of_value(l32 >> 1, half);
+    const float prior = t.prior(a, min(key, t.n - 1));  // (beside the keys' way)
+    float acc[16] = {};
+    const uint32_t k_rd = swz<HD>(l32, half);
+    // columns (user, head), 32 at a time
+    const int n_cols = (t.u1 - t.u0) * R;
+    for (int j0 = 0; j0 < n_cols; j0 += 32) {
+        const int j = min(j0 + l32, n_cols - 1);
+        const int b = t.user(a, t.u0 + j / R), q0 = a.cu_q[b];
+        const long row = max(0L, min((long)q0, a.total_q - 1));
+        const int head = t.g * R + j % R;
+        Frag<uint16_t, HD> q;
+        q.load(static_cast<const uint16_t*>(a.q) + ((size_t)row * a.n_q_heads + head) * HD, half);
+        float lse2 = a.lse[(size_t)head * a.total_q + row] * kLog2e;
+        if (a.cu_q[b + 1] - q0 != 1) lse2 = __builtin_nanf("");  // (a caller's size error shows)
+        if (j0 + l32 >= n_cols) lse2 = INFINITY;
+        __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): the keys are in LDS
+        f32x16 s = {};
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                *reinterpret_cast<const bf16x8*>(k_st + (k_rd ^ (uint32_t)(i << 5))), __builtin_bit_cast(bf16x8, q.w[i]),
+                s, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[r] += __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2, -lse2));
+    }
+    const float total = lane_totals<16>(acc, lane);
+    if (!(l32 & 1) && key < t.n) (t.ctx ? a.c_w : a.r_w)[t.row0 + key] = prior + total;
 }
 
 // The same for prompts in bf16, where products and exponentials count: a block
@@ -303,11 +358,6 @@ __global__ __launch_bounds__(256, 2) void weigh_prompt_kernel(const WeighArgs a)
             open(s);
         }
     };
-    auto uniform = [](const void* p) {
-        const uint64_t u = (uint64_t)p;
-        return (void*)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32) |
-                       (uint32_t)__builtin_amdgcn_readfirstlane((int)u));
-    };
     // c / R of a column c < CT + 8 from a row's first
     auto row_of = [&](int c) { return (int)(__umul24((uint32_t)c, a.inv_ratio) >> 16); };
     // Copies of a step's query rows, by the swizzle of the key tiles of prefill:
@@ -328,7 +378,7 @@ __global__ __launch_bounds__(256, 2) void weigh_prompt_kernel(const WeighArgs a)
         if (step_rem) find_offsets(s.rem);
         const int rows = min(s.n_rows - s.row0, CT);  // (CT columns span no more)
         const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
-            uniform(static_cast<const uint16_t*>(a.q) + ((size_t)(s.q0 + s.row0) * a.n_q_heads + g * R) * HD), (short)0,
+            uniform_ptr(static_cast<const uint16_t*>(a.q) + ((size_t)(s.q0 + s.row0) * a.n_q_heads + g * R) * HD), (short)0,
             __builtin_amdgcn_readfirstlane(((rows - 1) * a.n_q_heads + R) * ROWB), kBufferFlags);
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
@@ -475,17 +525,21 @@ long key_blocks(WeighArgs& a, int kt) {
 template <typename T, int HD>
 hipError_t launch(const WeighArgs& b, hipStream_t stream) {
     WeighArgs a = b;
-    const bool prompt = sizeof(T) == 2 && !a.one_query;
-    const long blocks = key_blocks(a, prompt ? 128 : 32 * Frag<T, HD>::kBlocks);
+    constexpr bool BF16 = sizeof(T) == 2;
+    const long blocks = key_blocks(a, BF16 ? (a.one_query ? 32 : 128) : 32);
     if (blocks <= 0) return hipSuccess;
     if (blocks > 0x7fffffffL) return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks);
-    if (prompt)
-        hipLaunchKernelGGL(weigh_prompt_kernel<HD>, grid, dim3(256), 0, stream, a);
-    else if (a.one_query)
-        hipLaunchKernelGGL((weigh_kernel<T, HD, 1>), grid, dim3(64), 0, stream, a);
-    else if constexpr (sizeof(T) == 4)
-        hipLaunchKernelGGL((weigh_kernel<T, HD, 4>), grid, dim3(256), 0, stream, a);
+    if constexpr (BF16) {
+        if (!a.one_query)
+            hipLaunchKernelGGL(weigh_prompt_kernel<HD>, grid, dim3(256), 0, stream, a);
+        else
+            hipLaunchKernelGGL(weigh_decode_kernel<HD>, grid, dim3(64), 0, stream, a);
+    } else if (a.one_query) {
+        hipLaunchKernelGGL((weigh_f32_kernel<HD, 1>), grid, dim3(64), 0, stream, a);
+    } else {
+        hipLaunchKernelGGL((weigh_f32_kernel<HD, 4>), grid, dim3(256), 0, stream, a);
+    }
     return hipGetLastError();
 }
 
