@@ -934,7 +934,7 @@ int recache_attend_quantized(int dtype, int layer, int n_layers, int n_req, cons
     const hipStream_t s = as_stream(stream);
     (void)hipGetLastError();
     if (max_q == 1) {
-        const int n_splits = decode_splits(n_req, n_kv_heads, max_kv > 0 ? max_kv : max_ctx);
+        const int n_splits = decode8_splits(n_req, n_kv_heads, max_kv > 0 ? max_kv : max_ctx);
         const size_t need = decode_workspace_bytes((long)n_req * n_splits, n_q_heads, head_dim);
         REQUIRE(workspace && workspace_bytes >= need, RECACHE_EWORKSPACE,
                 "decode needs a %zu-byte workspace, got %zu", need, workspace ? workspace_bytes : 0);

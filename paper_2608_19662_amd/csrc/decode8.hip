@@ -84,7 +84,8 @@ __device__ __forceinline__ uint64_t uniform64(uint64_t x) {
            (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
 }
 
-template <int HD>
+// NT: context rows are loaded with the non-temporal hint, as in decode.hip.
+template <int HD, bool NT>
 __global__ __launch_bounds__(kThreads, 2) void decode8_kernel(const Decode8Args a) {
     using T = DT8<HD>;
     __shared__ Dec8Smem sm;
@@ -185,8 +186,8 @@ __global__ __launch_bounds__(kThreads, 2) void decode8_kernel(const Decode8Args 
     int exps[2];  // lanes 0 .. 31: the tile's K exponent, others: V's
     int n_in[2];  // its keys
     int u_i = 0, u_lo = 0;  // wave-uniform walk over the segments: the current one, its first tile
-    auto load_tile = [&](auto buf_tag, int i) {
-        constexpr int buf = decltype(buf_tag)::value;
+    auto load_tile = [&](auto buf_tag, auto aux_tag, int i) {
+        constexpr int buf = decltype(buf_tag)::value, AUX = decltype(aux_tag)::value;
         const int t = t0 + wave + 4 * i;
         const bool seg = t < n_segt;
         long row, slot, rows;
@@ -228,12 +229,12 @@ __global__ __launch_bounds__(kThreads, 2) void decode8_kernel(const Decode8Args 
         for (int kb = 0; kb < T::NKB; ++kb)
 #pragma unroll
             for (int c = 0; c < T::NC; ++c)
-                kreg[buf][kb][c] = __builtin_amdgcn_raw_buffer_load_b128(kr, k_lane + kb * 16 * HD + c * 64, 0, 0);
+                kreg[buf][kb][c] = __builtin_amdgcn_raw_buffer_load_b128(kr, k_lane + kb * 16 * HD + c * 64, 0, AUX);
         char* dst = buf ? v_st1 : v_st0;
 #pragma unroll
         for (int j = 0; j < T::NJ; ++j)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_void*)(dst + j * 1024), 16,
-                                                     (int)(v_lane[(j * T::RPI >> 4) & 1] + j * 1024), 0, 0, 0);
+                                                     (int)(v_lane[(j * T::RPI >> 4) & 1] + j * 1024), 0, 0, AUX);
     };
 
     // ---- transpose reads: in a 16-lane group, lanes 2k and 2k + 1 point at the
@@ -323,28 +324,38 @@ __global__ __launch_bounds__(kThreads, 2) void decode8_kernel(const Decode8Args 
 
     // This wave's tiles are wave, wave + 4, ... of the range; the loads of the
     // next one are in flight while one is computed.
-    const int n_mine = t1 - t0 > wave ? (t1 - t0 - wave + 3) / 4 : 0;
-    if (n_mine > 0) {
-        load_tile(Tag<0>{}, 0);
-        for (int i = 0;; i += 2) {
-            if (i + 1 >= n_mine) {
-                __builtin_amdgcn_s_waitcnt(0x0F70);
-                compute(Tag<0>{});
-                break;
-            }
-            load_tile(Tag<1>{}, i + 1);
-            __builtin_amdgcn_s_waitcnt(T::WAIT_PREV);
-            compute(Tag<0>{});
-            if (i + 2 >= n_mine) {
-                __builtin_amdgcn_s_waitcnt(0x0F70);
-                compute(Tag<1>{});
-                break;
-            }
-            load_tile(Tag<0>{}, i + 2);
-            __builtin_amdgcn_s_waitcnt(T::WAIT_PREV);
-            compute(Tag<1>{});
-        }
+#define RC_TILES(AUX, FIRST, LAST)                            \
+    if (const int i0 = FIRST, i1 = LAST; i0 < i1) {           \
+        load_tile(Tag<0>{}, Tag<AUX>{}, i0);                  \
+        for (int i = i0;; i += 2) {                           \
+            if (i + 1 >= i1) {                                \
+                __builtin_amdgcn_s_waitcnt(0x0F70);           \
+                compute(Tag<0>{});                            \
+                break;                                        \
+            }                                                 \
+            load_tile(Tag<1>{}, Tag<AUX>{}, i + 1);           \
+            __builtin_amdgcn_s_waitcnt(T::WAIT_PREV);         \
+            compute(Tag<0>{});                                \
+            if (i + 2 >= i1) {                                \
+                __builtin_amdgcn_s_waitcnt(0x0F70);           \
+                compute(Tag<1>{});                            \
+                break;                                        \
+            }                                                 \
+            load_tile(Tag<0>{}, Tag<AUX>{}, i + 2);           \
+            __builtin_amdgcn_s_waitcnt(T::WAIT_PREV);         \
+            compute(Tag<1>{});                                \
+        }                                                     \
     }
+    auto tiles_of = [&](int n) { return n > wave ? (n - wave + 3) / 4 : 0; };
+    if constexpr (NT) {
+        // the resource tiles, then the context tiles with their own loads
+        const int n_res = max(0, min(t1, n_segt) - t0);
+        RC_TILES(0, 0, tiles_of(n_res))
+        RC_TILES(2, tiles_of(n_res), tiles_of(t1 - t0))
+    } else {
+        RC_TILES(0, 0, tiles_of(t1 - t0))
+    }
+#undef RC_TILES
 
     // ---- merge, as in decode.hip: the row groups of a head hold disjoint dims
     // of O^T and parts of its row sum; then the four waves, through LDS
@@ -384,13 +395,32 @@ __global__ __launch_bounds__(kThreads, 2) void decode8_kernel(const Decode8Args 
 
 }  // namespace
 
+// As many splits as decode.hip makes of half the keys, whose rows have twice the
+// bytes (12 requests of 60 to 9,000 context rows, 16 / 8 heads: 20.4 us instead of
+// 25.1 with all of its splits; one request over 3,400 keys 10.2 instead of 11.2, with
+// a third of them 11.4; the merge included).
+int decode8_splits(int n_req, int n_kv_heads, int max_kv) {
+    return decode_splits(n_req, n_kv_heads, max_kv / 2 + max_kv % 2);
+}
+
 hipError_t launch_decode8(const Decode8Args& a, hipStream_t s) {
     const long blocks = (long)a.d.n_req * a.d.n_kv_heads * a.d.n_splits;
     if (blocks > 0x7fffffffL || a.d.ratio < 1 || a.d.ratio > 16) return hipErrorInvalidValue;
-    if (a.d.head_dim == 128)
-        hipLaunchKernelGGL((decode8_kernel<128>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
-    else
-        hipLaunchKernelGGL((decode8_kernel<64>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
+    // context rows past the caches by the rule of decode.hip, on their bytes here
+    const bool nt = (unsigned long)std::min(a.d.c_rows, a.d.max_ctx_rows) * a.d.n_kv_heads * a.d.head_dim * 2 >=
+                    (512UL << 20);
+    const dim3 grid((unsigned)blocks), block(kThreads);
+    if (a.d.head_dim == 128) {
+        if (nt)
+            hipLaunchKernelGGL((decode8_kernel<128, true>), grid, block, 0, s, a);
+        else
+            hipLaunchKernelGGL((decode8_kernel<128, false>), grid, block, 0, s, a);
+    } else {
+        if (nt)
+            hipLaunchKernelGGL((decode8_kernel<64, true>), grid, block, 0, s, a);
+        else
+            hipLaunchKernelGGL((decode8_kernel<64, false>), grid, block, 0, s, a);
+    }
     const hipError_t err = hipGetLastError();
     return err != hipSuccess ? err : launch_decode_merge(a.d, s);
 }

@@ -179,6 +179,7 @@ struct Decode8Args : Cache8 {
     DecodeArgs d;
 };
 hipError_t launch_decode8(const Decode8Args& a, hipStream_t stream);
+int decode8_splits(int n_req, int n_kv_heads, int max_kv);  // at most decode_splits of the same
 
 struct Attn8Args : Cache8 {
     AttnArgs a;
