@@ -467,8 +467,14 @@ def attend_cached_noalloc(q, ctx_k, ctx_v, cu_q, cu_ctx, max_q: int, max_ctx: in
 
 # ------------------------------------------------ eviction by attention weight
 
+_F32 = None
+
+
 def _f32():
-    return (torch or _torch()).float32,
+    global _F32
+    if _F32 is None:
+        _F32 = ((torch or _torch()).float32,)
+    return _F32
 
 
 def resource_users(req_res_off, req_res, n_res: int, user_off, user_req, stream=None):
@@ -565,10 +571,27 @@ def select_kept(w, cu, cu_kept, kept_idx, *, max_len: int, kept_w=None, keep_fir
 
 # ------------------------------------------------------------- 8-bit caches
 
-def _codes(t, name, *dims):
-    """Device pointer of e4m3 codes (float8_e4m3fn, or their bytes as uint8)."""
-    _shape(t, name, *dims)
-    return _dev(t, name, ((torch or _torch()).float8_e4m3fn, torch.uint8))
+_CODES = None
+
+
+def _code_types():
+    """What codes may be held as: float8_e4m3fn, or their bytes as uint8."""
+    global _CODES
+    if _CODES is None:
+        _CODES = ((torch or _torch()).float8_e4m3fn, torch.uint8)
+    return _CODES
+
+
+def _ptr(t, name, dtypes):
+    """_dev of a tensor that has to be there, without a call per check."""
+    try:
+        if t.is_cuda and t.dtype in dtypes and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    if t is None:
+        raise TypeError("%s must be a CUDA tensor" % name)
+    return _dev(t, name, dtypes)
 
 
 def quantized_blocks(rows: int, n_seg: int) -> int:
@@ -603,8 +626,10 @@ def quantize_kv(k, v, k8, v8, k_exp, v_exp, cu, *, lens=None, cu_new=None, strea
     _numel(lens, "lens", n_seg)
     _numel(cu_new, "cu_new", n_seg + 1)
     blocks = rows // BLOCK_TOKENS + n_seg
+    _shape(v8, "v8", planes, rows, d)
     _shape(k_exp, "k_exp", planes, blocks)
     _shape(v_exp, "v_exp", planes, blocks)
+    u8, code = _u8(), _code_types()
     for t, name in ((k, "k"), (v, "v")):
         if not t.is_cuda:
             raise TypeError("%s must be a CUDA tensor" % name)
@@ -612,8 +637,8 @@ def quantize_kv(k, v, k8, v8, k_exp, v_exp, cu, *, lens=None, cu_new=None, strea
             raise ValueError("the elements of a row of %s must be contiguous" % name)
     _call("recache_quantize_kv", _dtype_code(k), n_seg, _dev(cu, "cu", _i32()), _dev(lens, "lens", _i32()), rows,
           planes, d, _dev(cu_new, "cu_new", _i32()), src_rows, k.data_ptr(), v.data_ptr(), row_stride, plane_stride,
-          _codes(k8, "k8", planes, rows, d), _codes(v8, "v8", planes, rows, d), _dev(k_exp, "k_exp", _u8()),
-          _dev(v_exp, "v_exp", _u8()), _stream(stream))
+          _ptr(k8, "k8", code), _ptr(v8, "v8", code), _ptr(k_exp, "k_exp", u8), _ptr(v_exp, "v_exp", u8),
+          _stream(stream))
 
 
 def attend_quantized(q, ctx_k, ctx_v, ctx_k_exp, ctx_v_exp, cu_q, cu_ctx, max_q: int, max_ctx: int, res_k, res_v,
@@ -624,48 +649,58 @@ def attend_quantized(q, ctx_k, ctx_v, ctx_k_exp, ctx_v_exp, cu_q, cu_ctx, max_q:
     [Hkv][rows][d] with exponents [Hkv][blocks], resources likewise, or a store
     [rows][d] with [blocks] (res_off).  ctx_len: context rows in use."""
     total_q, Hq, d = q.shape
-    if ctx_k.dim() != 3 or ctx_k.shape[2] != d:
-        raise ValueError("ctx_k must be [Hkv][rows][%d], has shape %s" % (d, tuple(ctx_k.shape)))
-    Hkv, ctx_rows = ctx_k.shape[0], ctx_k.shape[1]
+    ctx = ctx_k.shape
+    if len(ctx) != 3 or ctx[2] != d:
+        raise ValueError("ctx_k must be [Hkv][rows][%d], has shape %s" % (d, tuple(ctx)))
+    Hkv, ctx_rows, _ = ctx
     n_req = cu_q.numel() - 1
     n_res = cu_kept.numel() - 1
     E = n_req * n_layers * Hkv
     _same(q, out)
-    _shape(out, "out", total_q, Hq, d)
-    _shape(lse, "lse", Hq, total_q)
+    if out.shape != q.shape:
+        _shape(out, "out", total_q, Hq, d)
+    if lse is not None:
+        _shape(lse, "lse", Hq, total_q)
     _numel(cu_ctx, "cu_ctx", n_req + 1)
     _numel(ctx_len, "ctx_len", n_req)
     _numel(route_off, "route_off", E + 1)
     _numel(route_tokens, "route_tokens", E)
-    _shape(plan, "plan", n_layers, n_req * Hkv)
-    blocks = ctx_rows // BLOCK_TOKENS + n_req
-    _shape(ctx_k_exp, "ctx_k_exp", Hkv, blocks)
-    _shape(ctx_v_exp, "ctx_v_exp", Hkv, blocks)
+    if plan is not None:
+        _shape(plan, "plan", n_layers, n_req * Hkv)
+    exps = (Hkv, ctx_rows // BLOCK_TOKENS + n_req)
+    if ctx_v.shape != ctx or ctx_k_exp.shape != exps or ctx_v_exp.shape != exps:
+        _shape(ctx_v, "ctx_v", *ctx)
+        _shape(ctx_k_exp, "ctx_k_exp", *exps)
+        _shape(ctx_v_exp, "ctx_v_exp", *exps)
+    res = res_k.shape
     if res_off is not None:
         _numel(res_off, "res_off", n_res * Hkv + 1)
-        if res_k.dim() != 2 or res_k.shape[1] != d:
-            raise ValueError("a route-compacted store is [rows][%d], res_k has shape %s" % (d, tuple(res_k.shape)))
-        res_rows = res_k.shape[0]
-        exp_shape = (res_rows // BLOCK_TOKENS + n_res * Hkv,)
+        if len(res) != 2 or res[1] != d:
+            raise ValueError("a route-compacted store is [rows][%d], res_k has shape %s" % (d, tuple(res)))
+        res_rows = res[0]
+        exps = (res_rows // BLOCK_TOKENS + n_res * Hkv,)
     else:
-        if res_k.dim() != 3 or res_k.shape[0] != Hkv or res_k.shape[2] != d:
-            raise ValueError("res_k must be [%d][rows][%d], has shape %s" % (Hkv, d, tuple(res_k.shape)))
-        res_rows = res_k.shape[1]
-        exp_shape = (Hkv, res_rows // BLOCK_TOKENS + n_res)
-    _shape(res_k_exp, "res_k_exp", *exp_shape)
-    _shape(res_v_exp, "res_v_exp", *exp_shape)
+        if len(res) != 3 or res[0] != Hkv or res[2] != d:
+            raise ValueError("res_k must be [%d][rows][%d], has shape %s" % (Hkv, d, tuple(res)))
+        res_rows = res[1]
+        exps = (Hkv, res_rows // BLOCK_TOKENS + n_res)
+    if res_v.shape != res or res_k_exp.shape != exps or res_v_exp.shape != exps:
+        _shape(res_v, "res_v", *res)
+        _shape(res_k_exp, "res_k_exp", *exps)
+        _shape(res_v_exp, "res_v_exp", *exps)
+    i32, u8, code = _i32(), _u8(), _code_types()
+    dtype = _dtype_code(q)
+    float_type = (q.dtype,)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _call("recache_attend_quantized", _dtype_code(q), layer, n_layers, n_req, _dev(cu_q, "cu_q", _i32()),
-          _dev(cu_ctx, "cu_ctx", _i32()), _dev(ctx_len, "ctx_len", _i32()), total_q, int(max_q), int(max_ctx),
-          int(max_kv), int(max_route_len), Hq, Hkv, d, softmax_scale, _dev(q, "q"),
-          _codes(ctx_k, "ctx_k", Hkv, ctx_rows, d), _codes(ctx_v, "ctx_v", Hkv, ctx_rows, d),
-          _dev(ctx_k_exp, "ctx_k_exp", _u8()), _dev(ctx_v_exp, "ctx_v_exp", _u8()), ctx_rows,
-          _codes(res_k, "res_k", *res_k.shape), _codes(res_v, "res_v", *res_k.shape),
-          _dev(res_k_exp, "res_k_exp", _u8()), _dev(res_v_exp, "res_v_exp", _u8()), res_rows, n_res,
-          _dev(cu_kept, "cu_kept", _i32()), _dev(res_off, "res_off", _i32()), _dev(route_off, "route_off", _i32()),
-          _dev(route_res, "route_res", _i32()), _dev(route_tokens, "route_tokens", _i32()),
-          _dev(plan, "plan", _i32()), _dev(out, "out"), _dev(lse, "lse", _f32()), _dev(workspace, "workspace"),
-          ws_bytes, _stream(stream))
+    _call("recache_attend_quantized", dtype, layer, n_layers, n_req, _ptr(cu_q, "cu_q", i32),
+          _ptr(cu_ctx, "cu_ctx", i32), _dev(ctx_len, "ctx_len", i32), total_q, int(max_q), int(max_ctx), int(max_kv),
+          int(max_route_len), Hq, Hkv, d, softmax_scale, _ptr(q, "q", float_type), _ptr(ctx_k, "ctx_k", code),
+          _ptr(ctx_v, "ctx_v", code), _ptr(ctx_k_exp, "ctx_k_exp", u8), _ptr(ctx_v_exp, "ctx_v_exp", u8), ctx_rows,
+          _ptr(res_k, "res_k", code), _ptr(res_v, "res_v", code), _ptr(res_k_exp, "res_k_exp", u8),
+          _ptr(res_v_exp, "res_v_exp", u8), res_rows, n_res, _ptr(cu_kept, "cu_kept", i32),
+          _dev(res_off, "res_off", i32), _ptr(route_off, "route_off", i32), _ptr(route_res, "route_res", i32),
+          _ptr(route_tokens, "route_tokens", i32), _dev(plan, "plan", i32), _ptr(out, "out", float_type),
+          _dev(lse, "lse", _f32()), _dev(workspace, "workspace"), ws_bytes, _stream(stream))
 
 
 def check_offsets(cu, total: int, strict: bool = True) -> None:
