@@ -878,14 +878,34 @@ namespace {
 // A full grid with no bound on its keys (0) takes 8 waves.
 enum class PrefillForm { kSplit8, kSplit4, kBlocks4, kBlocks8 };
 
+long column_blocks(const AttnArgs& a) {
+    return std::max((a.lse_rows * a.ratio + 31) / 32, (long)a.n_units) * a.n_kv_heads;
+}
+
 PrefillForm prefill_form(const AttnArgs& a) {
-    const long col_blocks =
-        std::max((a.lse_rows * a.ratio + 31) / 32, (long)a.n_units) * a.n_kv_heads;
+    const long col_blocks = column_blocks(a);
     if (col_blocks <= 256) return PrefillForm::kSplit8;
     if (col_blocks <= 512 || (long)a.max_rows * a.ratio <= 32) return PrefillForm::kSplit4;
     if (col_blocks >= 2048 && (a.max_keys <= 0 || a.max_keys >= 4096)) return PrefillForm::kBlocks8;
     if (a.max_rows <= 32 && a.ratio > 4) return PrefillForm::kBlocks8;
     return PrefillForm::kBlocks4;
+}
+
+// The same over caches in 8 bits, where the split form (attn_split8.hip) reads half
+// the bytes and the block form converts each tile once per block, so that blocks of
+// 4 waves never win (us, split 8 waves / split 4 / blocks of 4 / blocks of 8):
+//   <= 256 column blocks: 28, 37, 134, 107 at 256
+//   <= 1,600, or a request's columns in one block: split with 4 waves: 102, 89,
+//       147, 120 at 1,024 (8 requests of 128 queries); 288, 271, 558, 645 at 1,024
+//       (64 of 16); 178, 159, 253, 185 at 1,500 (turns of 17 to 500 queries)
+//   more: blocks of 8 waves: 298, 230, 195, 193 at 1,800 (12 / 4 heads, head_dim
+//       64); 443, 405, 424, 313 at 2,048; 974, 759, 710, 553 at 16,384 over a
+//       pruned cache and 3,055, 2,719, 2,762, 2,058 over a whole one
+PrefillForm prefill_form8(const AttnArgs& a) {
+    const long col_blocks = column_blocks(a);
+    if (col_blocks <= 256) return PrefillForm::kSplit8;
+    if (col_blocks <= 1600 || (long)a.max_rows * a.ratio <= 32) return PrefillForm::kSplit4;
+    return PrefillForm::kBlocks8;
 }
 
 }  // namespace
@@ -906,11 +926,9 @@ hipError_t launch_attn_mfma(const AttnArgs& a, bool encode, int head_dim, hipStr
 
 hipError_t launch_attn8(const Attn8Args& a, int head_dim, hipStream_t stream) {
     if (a.a.ratio < 1 || a.a.max_rows < 1) return hipErrorInvalidValue;
-    switch (prefill_form(a.a)) {
+    switch (prefill_form8(a.a)) {
         case PrefillForm::kSplit8: return launch_attn_split8(a, head_dim, 8, stream);
         case PrefillForm::kSplit4: return launch_attn_split8(a, head_dim, 4, stream);
-        case PrefillForm::kBlocks4:
-            return head_dim == 128 ? launch<128, false, 4>(a, stream) : launch<64, false, 4>(a, stream);
         default: return head_dim == 128 ? launch<128, false, 8>(a, stream) : launch<64, false, 8>(a, stream);
     }
 }

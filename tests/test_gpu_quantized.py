@@ -138,6 +138,27 @@ def test_quantize_appends(dtype, layout):
         assert_same(*state, what=step)
 
 
+@pytest.mark.parametrize("dtype,d,planes,rows", [(torch.bfloat16, 128, 8, 90_000), (torch.float32, 64, 5, 180_001)])
+def test_quantize_many_rows(dtype, d, planes, rows):
+    """More than twice the last-level cache in one call, and plane by plane."""
+    g = torch.Generator(device=DEV).manual_seed(17)
+    k, v = (torch.randn(rows, planes, d, generator=g, device=DEV).to(dtype).transpose(0, 1) for _ in "kv")
+    assert k.numel() * 2 * (k.element_size() + 1) >= 512 << 20
+    cu = i32([0, 7, 7, rows // 2, rows])
+    blocks = rc.quantized_blocks(rows, 4)
+    one, many = ([torch.zeros(planes, rows, d, dtype=torch.uint8, device=DEV) for _ in "kv"]
+                 + [torch.zeros(planes, blocks, dtype=torch.uint8, device=DEV) for _ in "kv"] for _ in range(2))
+    rc.quantize_kv(k, v, *one, cu)
+    for p in range(planes):
+        rc.quantize_kv(k[p:p + 1], v[p:p + 1], *[t[p:p + 1] for t in many], cu)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(one, many))
+    n = 300  # and by the definition at the end
+    c, e = np.zeros((1, rows - rows // 2, d), np.uint8), np.zeros((1, blocks), np.uint8)
+    ref.quantize(v[-1:, rows // 2:].cpu().double().numpy(), c, e, np.array([0, rows - rows // 2]))
+    assert np.array_equal(bits(one[1])[-1, -n:], c[0, -n:])
+
+
 def test_quantize_values_that_are_not_finite():
     x = np.random.default_rng(3).normal(size=(1, 130, 128))
     x[0, 3, 4], x[0, 5, 6], x[0, 66, 0] = np.inf, np.nan, -np.inf
@@ -299,6 +320,21 @@ def test_attend_prefill_grids(Hq, Hkv, d, q, ctx):
     check_attend(out, lse, p.want(), "grid")
 
 
+@pytest.mark.parametrize("Hq,Hkv,d,q,ctx,store,slack", [
+    (32, 8, 128, [150] * 11 + [7], [150 + 37 * i for i in range(11)] + [500], False, 0),
+    (16, 2, 64, [470] * 7 + [1, 33], [470, 471, 500, 534, 600, 480, 512, 700, 40], True, 19),
+    (64, 8, 128, [1 + i % 9 for i in range(210)], [9 + i for i in range(210)], False, 0),  # many small requests
+])
+def test_attend_prefill_grids_of_blocks(Hq, Hkv, d, q, ctx, store, slack):
+    """More than 1,600 blocks of 32 columns."""
+    w = small_attend(78, len(q), 6, Hq, Hkv, d, "bf16", q, ctx, max_len=200)
+    p = Packed(w, 0, store, slack)
+    out, lse = p.run()
+    check_attend(out, lse, p.want(), "grid of blocks")
+    out2, lse2 = p.run(plan=p.rt.plan())
+    assert torch.equal(out, out2) and torch.equal(lse, lse2)
+
+
 @pytest.mark.parametrize("q", [1, 40])
 def test_attend_without_resources(q):
     """No request lists anything; no resource rows at all."""
@@ -405,6 +441,24 @@ def test_attend_sizes_that_understate():
     torch.cuda.synchronize()
     assert torch.isnan(out[40 + 64:].float()).all()
     check_attend(out[:104], lse[:, :104], (o[:104], l[:, :104], s[:104]), "understated")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_attend_large_context_planes(d):
+    """Contexts that may reach 512 MiB: the rows of the same short ones, at the
+    start of large planes, give the same bits."""
+    w = small_attend(43, 4, 5, 8, 2, d, "bf16", [1] * 4, [1, 200, 64, 333], max_len=200)
+    p = Packed(w, 0)
+    out, lse = p.run()
+    check_attend(out, lse, p.want(), "short planes")
+    rows = (512 << 20) // (2 * d * 2)
+    more = rc.quantized_blocks(rows, 4) - p.cke.shape[1]
+    grow = lambda t, n, x: torch.cat([t.view(torch.uint8), torch.full((2, n) + t.shape[2:], x, dtype=torch.uint8, device=DEV)], 1)
+    p.ck, p.cv = (grow(t, rows - t.shape[1], 0x7F).view(F8) for t in (p.ck, p.cv))
+    p.cke, p.cve = (grow(t, more, 240) for t in (p.cke, p.cve))
+    p.rt.max_ctx = rows // 4
+    out2, lse2 = p.run()
+    assert torch.equal(out, out2) and torch.equal(lse, lse2)
 
 
 def test_attend_plane_past_4_gib():
