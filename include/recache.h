@@ -487,8 +487,9 @@ int recache_attend_weights(int dtype, int layer, int n_layers, int n_req, const 
  *       its kept_idx are -1, its kept weights NaN)
  *   w[n_planes][total] fp32; kept_w[n_planes][total_kept] or NULL: the kept
  *       rows' weights, from which accumulation goes on over the pruned cache
- *   workspace: device scratch of recache_select_workspace_bytes(...) bytes
- *       (may be NULL when that is 0); contents need no initialisation
+ *   workspace: device scratch of recache_select_workspace_bytes(...) bytes,
+ *       8-byte aligned (may be NULL when that is 0); contents need no
+ *       initialisation
  * Errors: RECACHE_EINVAL for bad sizes or null pointers, RECACHE_EWORKSPACE.
  */
 size_t recache_select_workspace_bytes(int n_seg, int total, int max_len);

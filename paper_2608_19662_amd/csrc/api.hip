@@ -912,8 +912,8 @@ int recache_attend_quantized(int dtype, int layer, int n_layers, int n_req, cons
     if (rc_) return rc_;
     REQUIRE(dtype == RECACHE_BF16, RECACHE_EUNSUPPORTED, "8-bit caches are attended in bf16 only");
     REQUIRE(n_res >= 1, RECACHE_EINVAL, "n_res %d must be >= 1", n_res);
-    REQUIRE(ctx_k_exp && ctx_v_exp && ((res_k_exp && res_v_exp) || res_rows == 0), RECACHE_EINVAL,
-            "null scale pointer");
+    // (a store without rows has scale bytes as well: recache_quantized_blocks)
+    REQUIRE(ctx_k_exp && ctx_v_exp && res_k_exp && res_v_exp, RECACHE_EINVAL, "null scale pointer");
     REQUIRE((((uintptr_t)q | (uintptr_t)out | (uintptr_t)ctx_k | (uintptr_t)ctx_v | (uintptr_t)res_k |
               (uintptr_t)res_v) & 15) == 0,
             RECACHE_EINVAL, "q, out and the caches must be 16-byte aligned");

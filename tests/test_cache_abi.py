@@ -160,6 +160,7 @@ ATTEND = dict(dtype=1, layer=0, n_layers=1, n_req=2, cu_q=FAKE, cu_ctx=FAKE, ctx
     ("recache_attend_quantized", ATTEND, dict(res_rows=0), rc.EINVAL),
     ("recache_attend_quantized", ATTEND, dict(cke=None), rc.EINVAL),
     ("recache_attend_quantized", ATTEND, dict(rve=None), rc.EINVAL),
+    ("recache_attend_quantized", ATTEND, dict(res_rows=0, res_off=FAKE, rke=None), rc.EINVAL),
     ("recache_attend_quantized", ATTEND, dict(n_res=-1), rc.EINVAL),
     ("recache_attend_quantized", ATTEND, dict(n_res=0), rc.EINVAL),
     ("recache_attend_quantized", ATTEND, dict(plan=FAKE + 2), rc.EINVAL),

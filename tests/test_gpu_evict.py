@@ -166,6 +166,37 @@ def test_weights_of_a_decode_call_with_two_queries_are_nan():
     assert torch.isnan(rw[:, :int(w.cu_rows[1])]).all()
 
 
+@pytest.mark.parametrize("q", [1, 3])
+def test_weights_of_a_plane_past_4_gib(q):
+    """A context plane of 4.4 GB, the last rows of which are request 1's: as in a small one."""
+    d, rows, n = 128, 17_000_000, 300
+    if torch.cuda.mem_get_info()[0] < 8e9:
+        pytest.skip("needs 8 GB")
+    g = torch.Generator(device=DEV).manual_seed(5)
+    small = torch.zeros(1, 10 + n, d, dtype=torch.bfloat16, device=DEV)
+    small[:, 10:] = torch.randn(1, n, d, generator=g, device=DEV)
+    large = torch.zeros(1, rows, d, dtype=torch.bfloat16, device=DEV)
+    large[:, -n:] = small[:, 10:]
+    qq = torch.randn(1 + q, 4, d, generator=g, device=DEV).to(torch.bfloat16)
+    lse = torch.full((4, 1 + q), 3.0, device=DEV)
+    got = []
+    for k in (small, large):
+        w = torch.full(k.shape[:2], float("nan"), device=DEV)
+        rc.attend_weights(qq, lse, i32([0, 1, 1 + q]), i32([0, k.shape[1] - n, k.shape[1]]), q, None, None, None, None,
+                          0, ctx_k=k, ctx_w=w)
+        got.append(w)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0][:, -n:], got[1][:, -n:])
+    # rows of zeros: exp(-3) from each of the four heads
+    assert bool((got[1][:, :-n] == got[0][0, 0]).all()) and abs(float(got[0][0, 0]) - 4 * np.exp(-3)) < 1e-6
+    qf, kf = qq[1:].double(), small[0, 10:].double()
+    s = torch.einsum("ihd,jd->hij", qf.cpu(), kf.cpu()) / np.sqrt(d) - 3.0
+    seen = torch.arange(n)[None, :] <= torch.arange(q)[:, None] + n - q
+    want = torch.where(seen, s.exp(), 0.0).sum((0, 1)).numpy()
+    err = np.abs(f64(got[1][0, -n:]) - want)
+    assert (err <= (161e-6 + 4 * q * 2.0 ** -24) * want).all()
+
+
 def test_weights_from_the_librarys_own_lse():
     """The attention call's LSE is that of bf16-rounded weights: every query
     gives away 1, within 2^-8 and the fp32 terms."""
@@ -261,6 +292,24 @@ def test_select_long(lens):
         assert np.array_equal(idx, want)
         assert np.array_equal(kw, want_w)
         assert np.array_equal(run_select(w, cu, cu_kept, 4, 64, weights=False)[0], want)
+
+
+def test_select_weights_past_4_gib():
+    """Planes of 1.6 GB each, the last one past 2^32 bytes and its segment at their end."""
+    planes, total, n, k = 3, 400_000_000, 5000, 700
+    if torch.cuda.mem_get_info()[0] < 8e9:
+        pytest.skip("needs 8 GB")
+    rng = np.random.default_rng(11)
+    part = scores(rng, planes, n, "plain")
+    w = torch.zeros(planes, total, device=DEV)
+    w[:, -n:] = torch.from_numpy(part).to(DEV)
+    want, want_w = ref.select(part, prefix([n]), prefix([k]), 0, 1)
+    for max_len in (n, 20000):
+        idx, kw = torch.full((k,), -7, dtype=torch.int32, device=DEV), torch.zeros(planes, k, device=DEV)
+        ws = torch.empty(rc.select_workspace_bytes(2, total, max_len) or 1, dtype=torch.uint8, device=DEV)
+        rc.select_kept(w, i32([0, total - n, total]), i32([0, 0, k]), idx, max_len=max_len, kept_w=kw, workspace=ws)
+        torch.cuda.synchronize()
+        assert np.array_equal(idx.cpu().numpy(), want) and np.array_equal(kw.cpu().numpy(), want_w)
 
 
 def test_select_longer_than_max_len():
