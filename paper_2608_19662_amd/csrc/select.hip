@@ -78,16 +78,19 @@ __device__ __forceinline__ void row_keys(const SelectArgs& a, const Segment& seg
     for (int i = 0; i < N; ++i) keys[i] = seg.forced(row(i)) ? kForced : key_of((float)sum[i]);
 }
 
-// Sum over the 64 lanes, in every lane.
-__device__ __forceinline__ int wave_total(int x) {
+// Sum over the lanes up to each.
+__device__ __forceinline__ int wave_prefix(int x) {
     x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);  // row_shr:1, 2, 4, 8
     x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
     x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
     x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
     x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, true);  // row_bcast:15, into rows 1 and 3
     x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, true);  // row_bcast:31, into rows 2 and 3
-    return __builtin_amdgcn_readlane(x, 63);
+    return x;
 }
+
+// Sum over the 64 lanes, in every lane.
+__device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(wave_prefix(x), 63); }
 
 // The largest t in [lo, hi) with `need` keys or more at or above it, of the keys
 // that each(f) passes to f(key) (keys that do not count are 0).  There have to be as
@@ -405,11 +408,26 @@ __global__ __launch_bounds__(kLongWaves * 64) void kth_long_kernel(const SelectA
     if (seg.first + seg.last == seg.k) {
         t = kForced;
     } else if (in_bin > need_bin && in_bin <= kCandidates) {
-        each([&](int, int left, const uint32_t* k, int) {
+        // one LDS addition per wave and step: every lane's share lies together
+        for (int r0 = wave * kGroup; r0 < seg.len; r0 += NW * kGroup) {
+            uint32_t mine[kGroup / 64];
+            int n = 0;
+            chunk_keys<kGroup>(keys, r0, seg.len, lane, [&](int, int left, const uint32_t* k, int u) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e < left && k[e] >> kTopShift == bin) cand[atomicAdd(&n_cand, 1)] = k[e];
-        });
+                for (int e = 0; e < 4; ++e) {
+                    mine[u * 4 + e] = e < left ? k[e] : ~0u;  // (in the bin of forced rows, which is not searched)
+                    n += mine[u * 4 + e] >> kTopShift == bin;
+                }
+            });
+            int at = wave_prefix(n);
+            const int all = __builtin_amdgcn_readlane(at, 63);
+            int base = 0;
+            if (lane == 0) base = atomicAdd(&n_cand, all);
+            at += __builtin_amdgcn_readfirstlane(base) - n;
+#pragma unroll
+            for (int i = 0; i < kGroup / 64; ++i)
+                if (mine[i] >> kTopShift == bin) cand[at++] = mine[i];
+        }
         __syncthreads();
         t = kth_key<NW, true>(
             need_bin, lo, hi,
@@ -436,17 +454,16 @@ __global__ __launch_bounds__(kLongWaves * 64) void kth_long_kernel(const SelectA
     const int n_chunks = (seg.len + kChunk - 1) / kChunk;
     constexpr int C = kGroup / kChunk;
     for (int r0 = wave * kGroup; r0 < seg.len; r0 += NW * kGroup) {
-        int above[C] = {}, equal[C] = {};
+        int n[C] = {};  // above the k-th, and at it from bit 16 on
         chunk_keys<kGroup>(keys, r0, seg.len, lane, [&](int, int left, const uint32_t* k, int u) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                above[u * C / (kGroup / 256)] += __popcll(__builtin_amdgcn_ballot_w64(e < left && k[e] > t));
-                equal[u * C / (kGroup / 256)] += __popcll(__builtin_amdgcn_ballot_w64(e < left && k[e] == t));
-            }
+            for (int e = 0; e < 4; ++e) n[u * C / (kGroup / 256)] += e < left ? (k[e] > t) + ((k[e] == t) << 16) : 0;
         });
 #pragma unroll
-        for (int i = 0; i < C; ++i)
-            if (lane == 0 && r0 + i * kChunk < seg.len) before[r0 / kChunk + i] = make_int2(above[i], equal[i]);
+        for (int i = 0; i < C; ++i) {
+            const int sum = wave_total(n[i]);
+            if (lane == 0 && r0 + i * kChunk < seg.len) before[r0 / kChunk + i] = make_int2(sum & 0xffff, sum >> 16);
+        }
     }
     __syncthreads();
     int above = 0, equal = 0;
