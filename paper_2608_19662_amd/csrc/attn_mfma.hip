@@ -49,7 +49,13 @@
 // Caches in 8 bits (quant8.hpp; prefill only).  The same loop over bf16 tiles in LDS:
 // a thread fetches 16 bytes of codes of one row and its scale into registers
 // where the bf16 form starts its copy, and writes them to LDS as bf16 (exact) at
-// the tile's end, so that a code is converted once per block.
+// the tile's end, so that a code is converted once per block.  16,384 queries over
+// 8 resources and 2,048 context rows each, 32 / 8 heads: 1.91-2.05 ms (890-955 TFLOP/s)
+// against 1.56-1.68 of the bf16 form.  The conversion at the tile's end is what it
+// adds: every wave of the block is in it at once.  Beside the P V products it needs
+// registers that are not there (2.31 ms, spills).  S from the codes as they are, by
+// the 8-bit MFMA with block scales, with Q as two e4m3 matrices and V converted on
+// its way out of LDS, gained 1% at head_dim 128 and lost 5% at 64.
 //
 // Tiles never cross a resource boundary in encode, and the reduction order
 // depends only on local indices, so a resource's outputs are bit-identical

@@ -7,6 +7,9 @@
 // fragments are read: K 16 dims per 16-byte read, V by 8-bit transpose reads
 // (eight keys of one dim per lane).  At half the bytes both buffers of a wave
 // fit twice, and the next tile's copies are in flight for the whole of a tile.
+//
+// Bound by the latency of a wave's chain of tiles: 75 queries over 3,300 keys, 32 / 8
+// heads, 24 us (6.8 MB, and 80 blocks for 256 CUs).
 #include <algorithm>
 
 #include "attn_split.hpp"

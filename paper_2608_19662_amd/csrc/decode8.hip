@@ -10,9 +10,15 @@
 // resource's kept rows, or the context).  Its rows are one run of memory and
 // its two scales are uniform, so that a tile costs no per-key lookups: a
 // buffer resource whose extent is the tile (rows past its end read as zeros and
-// are masked; all of an offset is per lane, where it takes part in the check), constant offsets per lane, and the two scales as operands of the
-// conversions.  Segments end inside a tile now and then; what a partial tile
-// loses is matrix and vector work, which this kernel has to spare, no bytes.
+// are masked; all of an offset is per lane, where it takes part in the check),
+// constant offsets per lane, and the two scales as operands of the conversions.
+// Segments end inside a tile now and then; what a partial tile loses is matrix
+// and vector work, which this kernel has to spare, no bytes.
+//
+// 64 requests of 4,096 context rows over 32 resources each, 32 / 8 heads (887 MB):
+// 160 us with the merge, 5.5 TB/s; 12 requests of 60 to 9,000 context rows 20 us;
+// one request over 3,400 keys 8 us and 4 for the merge, each a chain of dependent
+// round trips.
 //
 // K dims are taken in the order in which 16-byte loads bring them: lane group
 // g holds dims 64 c + 16 g + [0, 16) in the two MFMA steps of chunk c, for K
