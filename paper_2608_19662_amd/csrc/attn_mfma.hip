@@ -412,11 +412,56 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void attn_mfma_kernel(const Args a
         u32x4 w[NF];
         uint32_t e[NF];
     };
-    // the tile set up last: row, slot and plane of this lane's fetches
+    // As above the stream is walked as runs, whose rows and scales are then at
+    // constant offsets from scalar pointers; a tile that crosses the end of one,
+    // or a run that the planes do not hold, takes row, slot and plane per lane.
+    int f_lo = 0, f_hi = 0;  // the current run's stream positions (f_hi 0: no run yet)
+    bool f_held = false;     // the planes hold it
+    const uint8_t *f_ck = nullptr, *f_cv = nullptr, *f_ke = nullptr, *f_ve = nullptr;
+    // the tile set up last
+    bool f_fast = false;
+    int f_at = 0;  // its first position in the run
     int f_row[NF] = {}, f_slot[NF] = {};
     uint32_t f_ctx = 0;
+    const int f_lane = wave * TL::RPW + lane / PPR;  // row of this lane's first fetch in the tile
     auto find_rows = [&](int kt) {
         if constexpr (Q8) {
+            const int p0 = kt * kBK;
+            if (p0 >= f_hi) {
+                const bool ctx = p0 >= s_vis;
+                int beg;
+                long slot;
+                if (!ctx) {
+                    while (p0 >= u_hi && u_sidx + 1 < n_seg)
+                        u_hi = __builtin_amdgcn_readfirstlane(sm.seg_start[++u_sidx + 1]);
+                    f_lo = __builtin_amdgcn_readfirstlane(sm.seg_start[u_sidx]);
+                    f_hi = u_hi;
+                    beg = __builtin_amdgcn_readfirstlane(sm.seg_row[u_sidx]);
+                    slot = __builtin_amdgcn_readfirstlane(sm.seg_slot[u_sidx]);
+                } else {
+                    f_lo = s_vis;
+                    f_hi = stream;
+                    beg = ctx_row0;
+                    slot = block_slot(ctx_row0, unit);
+                }
+                const long rows = ctx ? a.c_rows : a.k_rows, slots = ctx ? args.c_slots : args.r_slots;
+                const int len = f_hi - f_lo;
+                f_held = beg >= 0 && beg + (long)len <= rows && slot >= 0 && slot + (len + kBlk8 - 1) / kBlk8 <= slots;
+                auto uniform = [](const uint8_t* ptr) {
+                    const uint64_t u = (uint64_t)ptr;
+                    return (const uint8_t*)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32) |
+                                            (uint32_t)__builtin_amdgcn_readfirstlane((int)u));
+                };
+                const size_t row0 = ((size_t)g * (ctx ? a.c_rows : a.k_gstride) + beg) * HD;
+                const size_t slot0 = (size_t)g * (ctx ? args.c_slots : args.r_sstride) + slot;
+                f_ck = uniform((ctx ? args.ck : args.rk) + row0);
+                f_cv = uniform((ctx ? args.cv : args.rv) + row0);
+                f_ke = uniform((ctx ? args.ck_exp : args.rk_exp) + slot0);
+                f_ve = uniform((ctx ? args.cv_exp : args.rv_exp) + slot0);
+            }
+            f_fast = f_held && p0 + kBK <= f_hi;
+            f_at = p0 - f_lo;
+            if (f_fast) return;
             static_for<NF>([&](auto jc) {
                 constexpr int j = decltype(jc)::value;
                 const int p = min(kt * kBK + wave * TL::RPW + j * RPF + lane / PPR, stream - 1);
@@ -442,6 +487,21 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void attn_mfma_kernel(const Args a
     };
     auto fetch = [&](bool is_v, Fetched& f) {
         if constexpr (Q8) {
+            if (f_fast) {
+                const uint8_t* codes = (is_v ? f_cv : f_ck) + (size_t)f_at * HD;
+#pragma unroll
+                for (int j = 0; j < NF; ++j) {
+                    const uint32_t o = (uint32_t)((f_lane + j * RPF) * HD + lane % PPR * CB);
+                    if constexpr (CB == 16) {
+                        f.w[j] = *reinterpret_cast<const u32x4*>(codes + o);
+                    } else {
+                        const u32x2 w = *reinterpret_cast<const u32x2*>(codes + o);
+                        f.w[j][0] = w[0], f.w[j][1] = w[1];
+                    }
+                    f.e[j] = (is_v ? f_ve : f_ke)[(uint32_t)(f_at + f_lane + j * RPF) / kBlk8];
+                }
+                return;
+            }
 #pragma unroll
             for (int j = 0; j < NF; ++j) {
                 const bool ctx = (f_ctx >> j) & 1;
