@@ -46,16 +46,24 @@
 // across the loop, so that the registers spilled around the last tiles stay
 // few.
 //
-// Caches in 8 bits (quant8.hpp; prefill only).  The same loop over bf16 tiles in LDS:
-// a thread fetches 16 bytes of codes of one row and its scale into registers
-// where the bf16 form starts its copy, and writes them to LDS as bf16 (exact) at
-// the tile's end, so that a code is converted once per block.  16,384 queries over
-// 8 resources and 2,048 context rows each, 32 / 8 heads: 1.91-2.05 ms (890-955 TFLOP/s)
-// against 1.56-1.68 of the bf16 form.  The conversion at the tile's end is what it
-// adds: every wave of the block is in it at once.  Beside the P V products it needs
-// registers that are not there (2.31 ms, spills).  S from the codes as they are, by
-// the 8-bit MFMA with block scales, with Q as two e4m3 matrices and V converted on
-// its way out of LDS, gained 1% at head_dim 128 and lost 5% at 64.
+// Caches in 8 bits (quant8.hpp; prefill only).  The same loop; a thread fetches 16
+// bytes of codes of one row and its scale into registers where the bf16 form starts
+// its copy, and writes them to LDS at the tile's end:
+//     V as bf16 (exact), so that a code is converted once per block
+//     K as it is, beside its rows' scales.  S^T = K Q^T runs on the 32x32x64 e4m3
+//         MFMA with block scales, at twice the bf16 rate, with Q as the sum of two
+//         e4m3 matrices of a scale per row and 64 dims,
+//             q = q1 2^e + q2 2^(e - 4),
+//         formed once per block.  A bf16 query has 8 significant bits, 4 in each, so
+//         that it is taken exactly but for elements under 2^-13 of the largest of
+//         their 64 dims, which are off by at most 2^-21 of that one: as far as fp32
+//         sums of such products go.  The two products take the time of the bf16 one.
+// 16,384 queries over 8 resources and 2,048 context rows each, 32 / 8 heads: 1.76-1.81 ms, 1,010-1,040
+// TFLOP/s (the bf16 form: 1.56-1.68).
+// With K converted too 1.88 ms in the same run: every wave of the block is in the
+// tile's end at once, and beside the P V products the conversion needs registers that
+// are not there (spills).  V converted on its way out of LDS, by every wave, is slower
+// by 6% (16% at head_dim 64).
 //
 // Tiles never cross a resource boundary in encode, and the reduction order
 // depends only on local indices, so a resource's outputs are bit-identical
@@ -107,6 +115,8 @@ using u32v = uint32_t __attribute__((ext_vector_type(N)));
 template <int N>
 using u64v = uint64_t __attribute__((ext_vector_type(N)));
 
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef short s16x2 __attribute__((ext_vector_type(2)));
 template <int C>
 struct StageTag {
     static constexpr int value = C;
@@ -125,6 +135,7 @@ struct Smem {
 template <bool ENCODE, int NW>
 struct Smem8 : Smem<ENCODE, NW> {
     int seg_slot[kMaxSeg];  // first scale slot
+    uint8_t k_exp[2][kBK];  // of the K tiles' rows
 };
 
 template <typename Args>
@@ -542,6 +553,24 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void attn_mfma_kernel(const Args a
         }
     };
 
+    auto put_k = [&](const Fetched& f, auto stage_tag) {
+        if constexpr (Q8) {
+            constexpr int stage = decltype(stage_tag)::value;
+            char* buf = stage ? k_st1 : k_st0;
+#pragma unroll
+            for (int j = 0; j < NF; ++j) {
+                const int row = f_lane + j * RPF;
+                if constexpr (CB == 16) {
+                    *reinterpret_cast<u32x4*>(buf + row * HD + ((lane % PPR ^ k_mask8<HD>(row)) << 4)) = f.w[j];
+                } else {
+                    *reinterpret_cast<u32x2*>(buf + row * HD + ((lane % PPR / 2 ^ k_mask8<HD>(row)) << 4) +
+                                              lane % 2 * 8) = u32x2{f.w[j][0], f.w[j][1]};
+                }
+                if (lane % PPR == 0) sm.k_exp[stage][row] = (uint8_t)f.e[j];
+            }
+        }
+    };
+
     // Query rows first (they are needed first, for the RoPE), then the
     // prologue copies: K(0), V(0) into stage 0, K(1) into stage 1.  The
     // sources of tile 1 are kept for V(1) in the first loop iteration.
@@ -550,7 +579,7 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void attn_mfma_kernel(const Args a
         const uint16_t* qrow = a.q + ((size_t)(q_row0 + my_q_c) * a.n_q_heads + head) * HD;
 #pragma unroll
         for (int t = 0; t < TL::NT; ++t)
-            qraw[t] = *reinterpret_cast<const u32x4*>(qrow + t * 16 + half * 8);
+            qraw[t] = *reinterpret_cast<const u32x4*>(qrow + (Q8 ? t / 4 * 64 + half * 32 + t % 4 * 8 : t * 16 + half * 8));
     }
     Fetched f_k, f_v;  // K(t + 2) and V(t + 1) of 8-bit caches
     if constexpr (Q8) {
@@ -562,9 +591,9 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void attn_mfma_kernel(const Args a
             find_rows(1);
             fetch(false, f_k);
         }
-        put(f_k0, k_st0);
+        put_k(f_k0, StageTag<0>{});
         put(f_v, v_st0);
-        if (n_tiles > 1) put(f_k, k_st1);
+        if (n_tiles > 1) put_k(f_k, StageTag<1>{});
     } else {
         key_ptrs(0);
         copy(false, k_st0);
@@ -641,6 +670,50 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void attn_mfma_kernel(const Args a
 #pragma unroll
         for (int t = 0; t < TL::NT; ++t) qf[t] = __builtin_bit_cast(bf16x8, raw[t]);
     }
+    // 8-bit caches: the row as two e4m3 matrices, q1 2^e + q2 2^(e - 4), e for the 64
+    // dims of step c (this lane's are c*64 + half*32 + [0, 32)), by the rule of
+    // quantize.hip.  Both halves give the same scale, whichever of them an element of the
+    // product takes it from.
+    constexpr int NC = HD / 64;
+    v8i q1[NC], q2[NC];
+    int q_exps = 0;  // bytes: e of q1 and of q2 for each step
+    if constexpr (Q8) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            uint32_t most = 0;  // largest magnitude (bits of a float)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    most = max(most, max((qraw[c * 4 + i][w] & 0x7fffu) << 16, qraw[c * 4 + i][w] & 0x7fff0000u));
+            const auto both = __builtin_amdgcn_permlane32_swap(most, most, false, false);
+            most = max((uint32_t)both[0], (uint32_t)both[1]);
+            const bool finite = most < 0x7f800000u;
+            const int e1 = max(1, (int)(most >> 23) - 8 + ((most & 0x7fffffu) > 0x600000u ? 1 : 0));
+            const int e2 = max(1, e1 - 4);
+            q_exps |= (e1 | e2 << 8) << 16 * c;
+            const float s1 = block_scale((uint32_t)e1), s2 = block_scale((uint32_t)e2);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t lo = qraw[c * 4 + i / 2][i % 2 * 2], hi = qraw[c * 4 + i / 2][i % 2 * 2 + 1];
+                s16x2 w = {0, 0};
+                w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, lo), s1, false);
+                w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, hi), s1, true);
+                const uint32_t c1 = __builtin_bit_cast(uint32_t, w);
+                const uint32_t b0 = codes_to_bf16x2<false>(c1, s1), b1 = codes_to_bf16x2<true>(c1, s1);
+                auto rest = [](uint32_t q, uint32_t b, bool upper) {  // exact
+                    return upper ? __uint_as_float(q & 0xffff0000u) - __uint_as_float(b & 0xffff0000u)
+                                 : __uint_as_float(q << 16) - __uint_as_float(b << 16);
+                };
+                s16x2 v = {0, 0};
+                v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, rest(lo, b0, false), rest(lo, b0, true), s2, false);
+                v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, rest(hi, b1, false), rest(hi, b1, true), s2, true);
+                // (a row with an infinity or NaN has NaN logits)
+                q1[c][i] = finite ? (int)c1 : 0x7f7f7f7f;
+                q2[c][i] = finite ? __builtin_bit_cast(int, v) : 0;
+            }
+        }
+    }
 
     // LDS read offsets.  S^T operand A = K rows: key l32 (+32 for the second
     // block), chunk 2t + half.
@@ -667,8 +740,33 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void attn_mfma_kernel(const Args a
     };
 
     f32x16 sacc[2][2];  // S^T of two consecutive tiles, [tile & 1][key block]
-    auto qk = [&](f32x16* acc, const char* st) {
+    const uint32_t k8_rd0 = (uint32_t)(l32 * HD + (((half * 2) ^ k_mask8<HD>(l32)) << 4));
+    auto qk = [&](f32x16* acc, const char* st, const uint8_t* ke) {
         acc[0] = acc[1] = f32x16{};
+        if constexpr (Q8) {
+            const int e[2] = {ke[l32], ke[32 + l32]};
+            static_for<NC>([&](auto step) {
+                constexpr int c = decltype(step)::value;  // (the scales' bytes are immediates)
+                v8i kf[2];
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    const char* p = st + kb * 32 * HD;
+                    const u32x4 lo = *reinterpret_cast<const u32x4*>(p + (k8_rd0 ^ (uint32_t)(c << 6)));
+                    const u32x4 hi = *reinterpret_cast<const u32x4*>(p + (k8_rd0 ^ (uint32_t)(c << 6 | 16)));
+                    kf[kb] = v8i{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3],
+                                 (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+                }
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+                    acc[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf[kb], q1[c], acc[kb], 0, 0, 0, e[kb],
+                                                                              c * 2, q_exps);
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+                    acc[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf[kb], q2[c], acc[kb], 0, 0, 0, e[kb],
+                                                                              c * 2 + 1, q_exps);
+            });
+            return;
+        }
 #pragma unroll
         for (int t = 0; t < TL::NT; ++t)
 #pragma unroll
@@ -680,7 +778,9 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void attn_mfma_kernel(const Args a
 
     wait_vm0();
     __syncthreads();  // K(0), V(0), K(1) in LDS; RoPE table reads done
-    qk(sacc[0], k_st0);
+    const uint8_t* k_exps = nullptr;
+    if constexpr (Q8) k_exps = sm.k_exp[0];
+    qk(sacc[0], k_st0, k_exps);
     __syncthreads();  // every wave has read K(0) before K(2) is copied over it
 
     const float sl2 = a.scale_log2;
@@ -733,7 +833,7 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void attn_mfma_kernel(const Args a
         // the first tile sets the reference m (O and the row sum are still 0)
         if (kt == 0) m = row_max();
         // S(t + 1) on the matrix pipe while the weights of tile t are formed.
-        if constexpr (NEXT) qk(sacc[cur ^ 1], cur ? k_st0 : k_st1);
+        if constexpr (NEXT) qk(sacc[cur ^ 1], cur ? k_st0 : k_st1, Q8 ? k_exps + (cur ? 0 : kBK) : nullptr);
         // Weights relative to the reference m as it stands (no max of the
         // tile first), with this lane's sum of them as rounded for the P V
         // product, so that the output is an exact weighted mean of the V rows
@@ -762,13 +862,13 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void attn_mfma_kernel(const Args a
             // followed by an equal share of the ~96 VALU instructions that
             // form tile t's weights, so the matrix pipe and the VALU overlap
             // within this wave.
-            constexpr int NM = 2 * TL::NT, VPM = 96 / NM;
-            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            constexpr int NM = Q8 ? 4 * NC : 2 * TL::NT, VPM = 96 / NM, AHEAD = Q8 ? 6 : 2;
+            __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
 #pragma unroll
             for (int i = 0; i < NM; ++i) {
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
                 __builtin_amdgcn_sched_group_barrier(0x002, VPM, 0);
-                if (i + 2 < NM) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                if (i + AHEAD < (Q8 ? 4 * NC + 2 : NM)) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -816,7 +916,7 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void attn_mfma_kernel(const Args a
         if constexpr (NEXT) {
             if constexpr (Q8) {
                 put(f_v, cur ? v_st0 : v_st1);
-                if (kt + 2 < n_tiles) put(f_k, cur ? k_st1 : k_st0);
+                if (kt + 2 < n_tiles) put_k(f_k, StageTag<cur>{});
             } else {
                 wait_vm0();
             }
@@ -960,13 +1060,14 @@ PrefillForm prefill_form(const AttnArgs& a) {
 // The same over caches in 8 bits, where the split form (attn_split8.hip) reads half
 // the bytes and the block form converts each tile once per block, so that blocks of
 // 4 waves never win (us, split 8 waves / split 4 / blocks of 4 / blocks of 8):
-//   <= 256 column blocks: 28, 37, 134, 107 at 256
+//   <= 256 column blocks: 28, 37, 134, 94 at 256
 //   <= 1,600, or a request's columns in one block: split with 4 waves: 102, 89,
-//       147, 120 at 1,024 (8 requests of 128 queries); 288, 271, 558, 645 at 1,024
-//       (64 of 16); 178, 159, 253, 185 at 1,500 (turns of 17 to 500 queries)
-//   more: blocks of 8 waves: 298, 230, 195, 193 at 1,800 (12 / 4 heads, head_dim
-//       64); 443, 405, 424, 313 at 2,048; 974, 759, 710, 553 at 16,384 over a
-//       pruned cache and 3,055, 2,719, 2,762, 2,058 over a whole one
+//       147, 106 at 1,024 (8 requests of 128 queries); 288, 264, 558, 562 at 1,024
+//       (64 of 16); 178, 155, 253, 164 at 1,500 (turns of 17 to 500 queries)
+//   more: blocks of 8 waves: 298, 230, 195, 182 at 1,800 (12 / 4 heads, head_dim
+//       64); 443, 405, 424, 276 at 2,048; 974, 759, 710, 490 at 16,384 over a
+//       pruned cache and 3,055, 2,719, 2,762, 1,780 over a whole one
+// (blocks of 4 as they were when these converted K too)
 PrefillForm prefill_form8(const AttnArgs& a) {
     const long col_blocks = column_blocks(a);
     if (col_blocks <= 256) return PrefillForm::kSplit8;

@@ -44,13 +44,8 @@ union Split8Smem {
     float ml[W][kCols][2];
 };
 
-// Chunk swizzles of tile rows.  K: 16 consecutive rows of one chunk fall on
-// distinct banks; V: the 8 rows x 2 chunks that half a wave's transpose read
-// touches.
-template <int HD>
-__device__ __forceinline__ int k_mask8(int row) {
-    return HD == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
-}
+// Chunk swizzle of the V tile's rows: the 8 rows x 2 chunks that half a wave's
+// transpose read touches fall on distinct banks.
 template <int HD>
 __device__ __forceinline__ int vt_mask8(int row) {
     return HD == 128 ? (((row >> 1) & 1) << 1) | (((row >> 3) & 1) << 2) : ((row >> 3) & 1) << 1;

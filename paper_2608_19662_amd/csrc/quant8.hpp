@@ -32,4 +32,11 @@ __device__ __forceinline__ u32x4 codes_to_bf16x8(uint32_t lo, uint32_t hi, float
                  codes_to_bf16x2<false>(hi, scale), codes_to_bf16x2<true>(hi, scale)};
 }
 
+// Swizzle of the 16-byte chunks of K rows of codes in LDS: 16 consecutive rows of
+// one chunk fall on distinct banks.
+template <int HD>
+__device__ __forceinline__ int k_mask8(int row) {
+    return HD == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
+}
+
 }  // namespace rc

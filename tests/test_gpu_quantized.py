@@ -335,6 +335,32 @@ def test_attend_prefill_grids_of_blocks(Hq, Hkv, d, q, ctx, store, slack):
     assert torch.equal(out, out2) and torch.equal(lse, lse2)
 
 
+@pytest.mark.parametrize("Hq,Hkv,d,n", [(32, 8, 128, 11), (8, 8, 64, 44)])
+def test_attend_prefill_queries_of_uneven_size(Hq, Hkv, d, n):
+    """Dims of very different size within a query, more than 1,600 blocks of 32 columns.
+    Queries may be taken in parts that are off by up to 2^-21 of the largest of their 64 dims:
+    a logit by delta = scale 2^-21 sum over those 64 of (that largest * sum |k|), every
+    weight by it, the output by at most 2 delta of the mean distance."""
+    w = small_attend(79, n, 6, Hq, Hkv, d, "bf16", [150] * n, [150 + 17 * i for i in range(n)], max_len=200)
+    p = Packed(w, 0)
+    size = torch.ones(d, device=DEV)
+    size[:32], size[32:64] = 2.0 ** -9, 1.5
+    size[d - 7] = 6.0
+    size[d - 3], size[5] = 2.0 ** -12, 2.0 ** -20
+    p.q = (p.q.float() * size).to(torch.bfloat16)
+    out, lse = p.run()
+    o, l, spread = p.want()
+    qmax = p.q.float().abs().view(-1, Hq, d // 64, 64).amax(-1).amax((0, 1)).cpu().numpy()
+    ksum = max(np.abs(x).reshape(-1, d // 64, 64).sum(-1)[np.isfinite(x).reshape(-1, d).all(-1)].max(0).dot(qmax)
+               for x in (p.rk64, p.ck64))
+    delta = ksum * 2.0 ** -21 / np.sqrt(d)
+    assert delta < 1e-3
+    err = np.abs(f64(out) - o)
+    bound = (2.0 ** -8 * 1.005 + 7e-4 + 2 * delta) * spread + (2.0 ** -8 + 7e-4) * np.abs(o) + 1e-6
+    assert (err <= bound).all(), float((err / bound).max())
+    assert (np.abs(f64(lse) - l) <= np.log1p(2.0 ** -8) + 7e-4 + delta).all()
+
+
 @pytest.mark.parametrize("q", [1, 40])
 def test_attend_without_resources(q):
     """No request lists anything; no resource rows at all."""
