@@ -52,15 +52,9 @@
 //     V as bf16 (exact), so that a code is converted once per block
 //     K as it is, beside its rows' scales.  S^T = K Q^T runs on the 32x32x64 e4m3
 //         MFMA with block scales, at twice the bf16 rate, with Q as the sum of two
-//         e4m3 matrices of a scale per row and 64 dims,
-//             q = q1 2^e + q2 2^(e - 4),
-//         formed once per block.  A bf16 query has 8 significant bits, 4 in each, so
-//         that it is taken exactly but for elements under 2^-13 of the largest of
-//         their 64 dims, which are off by at most 2^-21 of that one: as far as fp32
-//         sums of such products go.  The two products take the time of the bf16 one.
-// 16,384 queries over 8 resources and 2,048 context rows each, 32 / 8 heads: 1.76-1.81 ms, 1,010-1,040
-// TFLOP/s (the bf16 form: 1.56-1.68).
-// With K converted too 1.88 ms in the same run: every wave of the block is in the
+//         e4m3 matrices (split_query): two products in the time of the bf16 one.
+// 16,384 queries over 8 resources and 2,048 context rows each, 32 / 8 heads: 1.76-1.81
+// ms, 1,010-1,040 TFLOP/s (the bf16 form: 1.56-1.68).  With K converted too 1.88 ms in the same run: every wave of the block is in the
 // tile's end at once, and beside the P V products the conversion needs registers that
 // are not there (spills).  V converted on its way out of LDS, by every wave, is slower
 // by 6% (16% at head_dim 64).
@@ -80,16 +74,6 @@
 namespace rc {
 
 namespace {
-
-// f(integral_constant<int, i>) for i = 0 .. N-1, unrolled at compile time.
-template <typename F, int... I>
-__device__ __forceinline__ void static_for_impl(F&& f, std::integer_sequence<int, I...>) {
-    (f(std::integral_constant<int, I>{}), ...);
-}
-template <int N, typename F>
-__device__ __forceinline__ void static_for(F&& f) {
-    static_for_impl(f, std::make_integer_sequence<int, N>{});
-}
 
 constexpr int kBK = 64;  // keys per tile
 template <int HD, int NW>
@@ -115,8 +99,6 @@ using u32v = uint32_t __attribute__((ext_vector_type(N)));
 template <int N>
 using u64v = uint64_t __attribute__((ext_vector_type(N)));
 
-typedef int v8i __attribute__((ext_vector_type(8)));
-typedef short s16x2 __attribute__((ext_vector_type(2)));
 template <int C>
 struct StageTag {
     static constexpr int value = C;
@@ -670,49 +652,13 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void attn_mfma_kernel(const Args a
 #pragma unroll
         for (int t = 0; t < TL::NT; ++t) qf[t] = __builtin_bit_cast(bf16x8, raw[t]);
     }
-    // 8-bit caches: the row as two e4m3 matrices, q1 2^e + q2 2^(e - 4), e for the 64
-    // dims of step c (this lane's are c*64 + half*32 + [0, 32)), by the rule of
-    // quantize.hip.  Both halves give the same scale, whichever of them an element of the
-    // product takes it from.
+    // 8-bit caches: the row as two e4m3 matrices, in 64-dim steps
     constexpr int NC = HD / 64;
     v8i q1[NC], q2[NC];
     int q_exps = 0;  // bytes: e of q1 and of q2 for each step
     if constexpr (Q8) {
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            uint32_t most = 0;  // largest magnitude (bits of a float)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int w = 0; w < 4; ++w)
-                    most = max(most, max((qraw[c * 4 + i][w] & 0x7fffu) << 16, qraw[c * 4 + i][w] & 0x7fff0000u));
-            const auto both = __builtin_amdgcn_permlane32_swap(most, most, false, false);
-            most = max((uint32_t)both[0], (uint32_t)both[1]);
-            const bool finite = most < 0x7f800000u;
-            const int e1 = max(1, (int)(most >> 23) - 8 + ((most & 0x7fffffu) > 0x600000u ? 1 : 0));
-            const int e2 = max(1, e1 - 4);
-            q_exps |= (e1 | e2 << 8) << 16 * c;
-            const float s1 = block_scale((uint32_t)e1), s2 = block_scale((uint32_t)e2);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t lo = qraw[c * 4 + i / 2][i % 2 * 2], hi = qraw[c * 4 + i / 2][i % 2 * 2 + 1];
-                s16x2 w = {0, 0};
-                w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, lo), s1, false);
-                w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, hi), s1, true);
-                const uint32_t c1 = __builtin_bit_cast(uint32_t, w);
-                const uint32_t b0 = codes_to_bf16x2<false>(c1, s1), b1 = codes_to_bf16x2<true>(c1, s1);
-                auto rest = [](uint32_t q, uint32_t b, bool upper) {  // exact
-                    return upper ? __uint_as_float(q & 0xffff0000u) - __uint_as_float(b & 0xffff0000u)
-                                 : __uint_as_float(q << 16) - __uint_as_float(b << 16);
-                };
-                s16x2 v = {0, 0};
-                v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, rest(lo, b0, false), rest(lo, b0, true), s2, false);
-                v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, rest(hi, b1, false), rest(hi, b1, true), s2, true);
-                // (a row with an infinity or NaN has NaN logits)
-                q1[c][i] = finite ? (int)c1 : 0x7f7f7f7f;
-                q2[c][i] = finite ? __builtin_bit_cast(int, v) : 0;
-            }
-        }
+        for (int c = 0; c < NC; ++c) q_exps |= split_query(qraw + c * 4, q1[c], q2[c]) << 16 * c;
     }
 
     // LDS read offsets.  S^T operand A = K rows: key l32 (+32 for the second

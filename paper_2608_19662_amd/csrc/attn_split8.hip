@@ -3,13 +3,15 @@
 //
 // As in decode8.hip a tile lies in one scale block (here 32 of its 64 rows),
 // so that its rows are one run of memory and its two scales are operands of the
-// conversions.  Codes go into LDS as they are and become bf16 as the MFMA
-// fragments are read: K 16 dims per 16-byte read, V by 8-bit transpose reads
-// (eight keys of one dim per lane).  At half the bytes both buffers of a wave
-// fit twice, and the next tile's copies are in flight for the whole of a tile.
+// products.  Codes go into LDS as they are.  K's go into the 32x32x64 e4m3 MFMA
+// with block scales as they are, with Q as two e4m3 matrices (split_query); V's become
+// bf16 as the fragments are read, by 8-bit transpose reads (eight keys of one dim
+// per lane).  At half the bytes both buffers of a wave fit twice, and the next tile's
+// copies are in flight for the whole of a tile.
 //
 // Bound by the latency of a wave's chain of tiles: 75 queries over 3,300 keys, 32 / 8
-// heads, 24 us (6.8 MB, and 80 blocks for 256 CUs).
+// heads, 24-25 us (7.3 MB, and 80 blocks for 256 CUs); 8 requests of 128 queries
+// over the same 87 (90 with K converted as well).
 #include <algorithm>
 
 #include "attn_split.hpp"
@@ -56,8 +58,7 @@ __global__ __launch_bounds__(W * 64, 2) void attn_split8_kernel(const Attn8Args 
     const AttnArgs& a = x.a;
     constexpr int kThreads = W * 64;
     constexpr int CPR = HD / 16;       // 16-byte chunks per row
-    constexpr int NT = HD / 16;        // MFMA k-steps over head_dim
-    constexpr int NC = HD / 32;        // 16-byte K reads per lane (two steps each)
+    constexpr int NC = HD / 64;        // 64-dim steps of S^T
     constexpr int NDB = HD / 32;       // 32-wide blocks of head_dim
     constexpr int RPI = 64 / CPR;      // rows per 1 KB wave copy
     constexpr int NJ = kKeys / RPI;    // copies per K or V tile
@@ -112,15 +113,19 @@ __global__ __launch_bounds__(W * 64, 2) void attn_split8_kernel(const Attn8Args 
     const int my_row = my_j / R, my_head = g * R + my_j % R;
     const int first_row = j0 / R, last_row = (j0 + used - 1) / R;
 
-    // ---- Q^T (B operand) in K's order of dims: step t holds dims
-    // (t / 2) * 32 + half * 16 + (t % 2) * 8 + [0, 8) of this lane's column
-    bf16x8 qf[NT];
+    // ---- Q^T (B operand): this lane's column as two e4m3 matrices, in 64-dim steps
+    v8i q1[NC], q2[NC];
+    int q_exps = 0;  // bytes: their exponents for each step
     {
         const long row = max(0L, min((long)q_row0 + my_row, a.lse_rows - 1));
-        const uint16_t* qp = a.q + ((size_t)row * a.n_q_heads + my_head) * HD + half * 16;
+        const uint16_t* qp = a.q + ((size_t)row * a.n_q_heads + my_head) * HD + half * 32;
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-            qf[t] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qp + (t >> 1) * 32 + (t & 1) * 8));
+        for (int c = 0; c < NC; ++c) {
+            u32x4 raw[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) raw[i] = *reinterpret_cast<const u32x4*>(qp + c * 64 + i * 8);
+            q_exps |= split_query(raw, q1[c], q2[c]) << 16 * c;
+        }
     }
 
     // ---- visible segments of this (request, layer, group), in tiles
@@ -225,8 +230,8 @@ __global__ __launch_bounds__(W * 64, 2) void attn_split8_kernel(const Attn8Args 
             __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_void*)(dst + TILEB + j * 1024), 16, (int)v_lane[j], 0, 0, 0);
     };
 
-    // K as the A operand: key l32, chunk 2c + half
-    const uint32_t k_rd0 = (uint32_t)(l32 * HD + ((half ^ k_mask8<HD>(l32)) << 4));
+    // K as the A operand: key l32, chunks 4c + 2 half + {0, 1}
+    const uint32_t k_rd0 = (uint32_t)(l32 * HD + (((half * 2) ^ k_mask8<HD>(l32)) << 4));
     // V^T transpose reads: in a 16-lane group G, lanes 2k and 2k + 1 point at the
     // two halves of row k's chunk, and lane i receives column i of the 8 rows:
     // rows s*16 + w*8 + half*4 + [0, 4) (w = 0, 1), the keys that P^T holds in
@@ -247,19 +252,19 @@ __global__ __launch_bounds__(W * 64, 2) void attn_split8_kernel(const Attn8Args 
 
     auto compute = [&](auto buf_tag, int t) {
         constexpr int buf = decltype(buf_tag)::value;
-        const float ksc = block_scale((uint32_t)__builtin_amdgcn_readlane(exps[buf], 0));
+        const int ke = __builtin_amdgcn_readlane(exps[buf], 0);
         const float vsc = block_scale((uint32_t)__builtin_amdgcn_readlane(exps[buf], 32));
         const char* kb = buf ? st1[wave] : st0[wave];
         const char* vb = kb + TILEB;
         f32x16 sc = {};
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const u32x4 w = *reinterpret_cast<const u32x4*>(kb + (k_rd0 ^ (uint32_t)(c << 5)));
-            sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, codes_to_bf16x8(w[0], w[1], ksc)),
-                                                         qf[2 * c], sc, 0, 0, 0);
-            sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, codes_to_bf16x8(w[2], w[3], ksc)),
-                                                         qf[2 * c + 1], sc, 0, 0, 0);
-        }
+        static_for<NC>([&](auto step) {
+            constexpr int c = decltype(step)::value;
+            const u32x4 lo = *reinterpret_cast<const u32x4*>(kb + (k_rd0 ^ (uint32_t)(c << 6)));
+            const u32x4 hi = *reinterpret_cast<const u32x4*>(kb + (k_rd0 ^ (uint32_t)(c << 6 | 16)));
+            const v8i kf = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+            sc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, q1[c], sc, 0, 0, 0, ke, c * 2, q_exps);
+            sc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kf, q2[c], sc, 0, 0, 0, ke, c * 2 + 1, q_exps);
+        });
         // key offsets that every column of the block sees, and this lane's
         const bool seg = t < n_segt;
         const int p0 = (t - n_segt) * kKeys;  // (causal tiles)

@@ -4,7 +4,9 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+
 #include <stdint.h>
+#include <utility>
 
 namespace rc {
 
@@ -154,6 +156,16 @@ __device__ __forceinline__ int find_segment(const int32_t* cu, int n, int unit, 
         hi = min(hi, lo + step);
     }
     return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// f(integral_constant<int, i>) for i = 0 .. N-1, unrolled at compile time.
+template <typename F, int... I>
+__device__ __forceinline__ void static_for_impl(F&& f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void static_for(F&& f) {
+    static_for_impl(f, std::make_integer_sequence<int, N>{});
 }
 
 }  // namespace rc

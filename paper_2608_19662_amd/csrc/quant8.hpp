@@ -39,4 +39,48 @@ __device__ __forceinline__ int k_mask8(int row) {
     return HD == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
 }
 
+// A bf16 query row for the 32x32x64 e4m3 MFMA, as the sum of two e4m3 matrices:
+//     q = q1 2^(e - 127) + q2 2^(e - 4 - 127)
+// with e as quantize.hip takes it, of 64 dims.  A bf16 value has 8 significant bits, 4
+// in each, so that it is taken exactly but where it is under 2^-13 of the largest of
+// the 64: then it is off by at most 2^-21 of that one, about as far as fp32 sums of
+// such products go.
+// raw: this lane's 32 of the dims (half * 32 + [0, 32)); returns the two exponents as
+// bytes 0 and 1.  Both halves give the same ones, whichever of them an element of the
+// product takes its scale from.
+typedef int v8i __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ int split_query(const u32x4* raw, v8i& q1, v8i& q2) {
+    typedef short s16x2 __attribute__((ext_vector_type(2)));
+    uint32_t most = 0;  // largest magnitude (bits of a float)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) most = max(most, max((raw[i][w] & 0x7fffu) << 16, raw[i][w] & 0x7fff0000u));
+    const auto both = __builtin_amdgcn_permlane32_swap(most, most, false, false);
+    most = max((uint32_t)both[0], (uint32_t)both[1]);
+    const bool finite = most < 0x7f800000u;
+    const int e1 = max(1, (int)(most >> 23) - 8 + ((most & 0x7fffffu) > 0x600000u ? 1 : 0));
+    const int e2 = max(1, e1 - 4);
+    const float s1 = block_scale((uint32_t)e1), s2 = block_scale((uint32_t)e2);
+    auto rest = [](uint32_t q, uint32_t b, bool upper) {  // exact
+        return upper ? __uint_as_float(q & 0xffff0000u) - __uint_as_float(b & 0xffff0000u)
+                     : __uint_as_float(q << 16) - __uint_as_float(b << 16);
+    };
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t lo = raw[i / 2][i % 2 * 2], hi = raw[i / 2][i % 2 * 2 + 1];
+        s16x2 w = {0, 0}, v = {0, 0};
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, lo), s1, false);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, hi), s1, true);
+        const uint32_t c1 = __builtin_bit_cast(uint32_t, w);
+        const uint32_t b0 = codes_to_bf16x2<false>(c1, s1), b1 = codes_to_bf16x2<true>(c1, s1);
+        v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, rest(lo, b0, false), rest(lo, b0, true), s2, false);
+        v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, rest(hi, b1, false), rest(hi, b1, true), s2, true);
+        // (a row with an infinity or NaN has NaN logits)
+        q1[i] = finite ? (int)c1 : 0x7f7f7f7f;
+        q2[i] = finite ? __builtin_bit_cast(int, v) : 0;
+    }
+    return e1 | e2 << 8;
+}
+
 }  // namespace rc

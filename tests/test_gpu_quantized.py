@@ -335,9 +335,9 @@ def test_attend_prefill_grids_of_blocks(Hq, Hkv, d, q, ctx, store, slack):
     assert torch.equal(out, out2) and torch.equal(lse, lse2)
 
 
-@pytest.mark.parametrize("Hq,Hkv,d,n", [(32, 8, 128, 11), (8, 8, 64, 44)])
+@pytest.mark.parametrize("Hq,Hkv,d,n", [(32, 8, 128, 11), (8, 8, 64, 44), (32, 8, 128, 2), (8, 8, 64, 4)])
 def test_attend_prefill_queries_of_uneven_size(Hq, Hkv, d, n):
-    """Dims of very different size within a query, more than 1,600 blocks of 32 columns.
+    """Dims of very different size within a query, large grids and small.
     Queries may be taken in parts that are off by up to 2^-21 of the largest of their 64 dims:
     a logit by delta = scale 2^-21 sum over those 64 of (that largest * sum |k|), every
     weight by it, the output by at most 2 delta of the mean distance."""
