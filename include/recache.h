@@ -542,7 +542,10 @@ int recache_quantize_kv(int dtype, int n_seg, const int32_t* cu, const int32_t* 
 /*
  * recache_attend_cached over 8-bit caches, resource rows and context alike
  * (bf16 queries and outputs).  The result is that of the call on the caches'
- * values in bf16, up to the order of the sums.  Beside its arguments:
+ * values in bf16, up to the order of the sums and, with max_q > 1, the smallest
+ * elements of a query: one under 2^-13 of the largest of its 64 dims (of 0 ..
+ * 63, of 64 .. 127) is taken to within 2^-21 of that largest one.  Beside its
+ * arguments:
  *   ctx_k/ctx_v, ctx_k_exp/ctx_v_exp: planes of ctx_rows rows, segments cu_ctx
  *   ctx_len[n_req] (device int32) or NULL: context rows in use, Tc_b =
  *       ctx_len[b] <= cu_ctx[b+1] - cu_ctx[b], so that contexts grow in place;

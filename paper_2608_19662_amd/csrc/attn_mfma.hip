@@ -54,10 +54,11 @@
 //         MFMA with block scales, at twice the bf16 rate, with Q as the sum of two
 //         e4m3 matrices (split_query): two products in the time of the bf16 one.
 // 16,384 queries over 8 resources and 2,048 context rows each, 32 / 8 heads: 1.61-1.81
-// ms by the GPU's state, 1,010-1,140 TFLOP/s (the bf16 form: 1.56-1.68).  With K converted too 1.88 ms in the same run: every wave of the block is in the
-// tile's end at once, and beside the P V products the conversion needs registers that
-// are not there (spills).  V converted on its way out of LDS, by every wave, is slower
-// by 6% (16% at head_dim 64).
+// ms by the GPU's state, 1,010-1,140 TFLOP/s (the bf16 form: 1.56-1.68).  With K
+// converted too it was 6% slower: every wave of the block is in the tile's end at
+// once, and beside the P V products the conversion needs registers that are not there
+// (spills).  V converted on its way out of LDS, by every wave, costs 6% (16% at
+// head_dim 64).
 //
 // Tiles never cross a resource boundary in encode, and the reduction order
 // depends only on local indices, so a resource's outputs are bit-identical
